@@ -29,6 +29,7 @@
 #ifndef TBS_H
 #define TBS_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -403,6 +404,149 @@ tbs_status tbs_transducer_forward(int32_t kind, const float *blank, const float 
                                   const int32_t *lengths, int32_t B, int32_t T, int32_t U,
                                   double *out_total, float *out_alpha, int32_t *out_status,
                                   void *hip_stream);
+
+/*
+ * Gradient of the log-likelihoods of tbs_transducer_forward with respect to blank and
+ * label (training: gradients of the losses of Sec. 3): the derivative of
+ * sum_b weights[b] total[b].
+ *   kind, blank, label, lengths, B, T, U, out_total, out_status as tbs_transducer_forward;
+ *   weights         DEVICE double [B] or NULL (1 each): the derivative of what the caller
+ *                   minimises with respect to total[b], for example -1 / B;
+ *   out_grad_blank  DEVICE float [B][T][U+1], out_grad_label DEVICE float [B][T][U]: fully
+ *                   written, 0 outside an utterance's lengths.  0 throughout an utterance
+ *                   that no path leads through (total -inf, or below -1e8, where the scores
+ *                   no longer tell its paths apart) and one with lengths out of range; NaN
+ *                   inside the lengths of one whose total is NaN or above 1e8.  Scores are
+ *                   held with fp32 mantissas and integer exponents (recursions in fp64), so
+ *                   a gradient is within a few 1e-7 of itself however long the utterance;
+ *   workspace       DEVICE, 16-byte aligned, of at least the bytes that
+ *                   tbs_transducer_gradient_workspace gives for B, T and U; contents on
+ *                   entry are of no matter.  Calls that may overlap need one each.
+ * Errors: as tbs_transducer_forward; TBS_EINVAL for a workspace that is too small or not
+ * aligned.
+ */
+size_t tbs_transducer_gradient_workspace(int32_t B, int32_t T, int32_t U);
+tbs_status tbs_transducer_gradient(int32_t kind, const float *blank, const float *label,
+                                   const int32_t *lengths, const double *weights, int32_t B,
+                                   int32_t T, int32_t U, double *out_total,
+                                   float *out_grad_blank, float *out_grad_label,
+                                   int32_t *out_status, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream);
+
+/*
+ * Linear layers with a fused epilogue (the projections and the output layer of a joiner:
+ * tanh(x W^T + bias + dec), then h W^T + bias) and their gradients.  A matrix is a device
+ * pointer to rows of `ld` elements each, ld at least the row's width; pointers need the
+ * alignment of their elements only.  All matrices of a call have one element type; sums are
+ * fp32, a result is rounded once.
+ */
+typedef enum { TBS_F32 = 0, TBS_BF16 = 1, TBS_F16 = 2 } tbs_dtype;
+typedef enum {
+  TBS_ACT_NONE = 0,
+  TBS_ACT_RELU = 1,
+  TBS_ACT_TANH = 2,
+  TBS_ACT_SILU = 3,  /* z / (1 + e^-z) */
+  TBS_ACT_GELU = 4   /* z (1 + erf(z / sqrt 2)) / 2 */
+} tbs_activation;
+
+/*
+ * out = act(x w^T + bias + residual), or with residual_after act(x w^T + bias) + residual.
+ *   x [M][K], w [N][K] (torch Linear layout), bias [N] or NULL; residual [M][N] or NULL
+ *   (ld 0: one row for all m); out [M][N]; pre [M][N] or NULL: receives the activation's
+ *   argument, which tbs_linear_backward needs.  M >= 0 (0 is a no-op), N, K >= 1.  out may
+ *   be the residual itself (same rows); otherwise the outputs overlap nothing.
+ *   workspace  DEVICE, 16-byte aligned, of at least the bytes that tbs_linear_workspace
+ *              gives (0: none, may be NULL); calls that may overlap need one each.
+ * The order of the sums depends on M, N, K, dtype and the current device only: the same
+ * inputs give the same bits.
+ * Errors: TBS_EINVAL for unknown dtype or activation, sizes, NULL pointers, a row length
+ * below the width or a workspace that is too small; TBS_ECAPACITY for more than 2^23 tiles
+ * of 64 x 64 results or a dimension above 2^30.
+ */
+size_t tbs_linear_workspace(int32_t dtype, int32_t M, int32_t N, int32_t K);
+tbs_status tbs_linear(int32_t dtype, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                      const void *bias, const void *residual, int64_t ldr,
+                      int32_t residual_after, int32_t activation, int32_t M, int32_t N,
+                      int32_t K, void *out, int64_t ldo, void *pre, int64_t ldp,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradients of tbs_linear from grad_out [M][N], the gradient of out:
+ *   dz    [M][N] = grad_out * act'(pre): the gradient of the activation's argument, so of
+ *         a residual added before it; rounded to the element type, as the products below
+ *         take it.  Not written for TBS_ACT_NONE (dz is grad_out then);
+ *   dx    [M][K] = dz w;  dw [N][K] = dz^T x;  dbias [N] = the sum of dz's rows.
+ * (The gradient of a residual added after the activation is grad_out.)
+ *   pre   [M][N] as tbs_linear wrote it; NULL for TBS_ACT_NONE.
+ *   dx, dw, dbias, dz may each be NULL (not wanted; w is not read without dx, x not without
+ *   dw).  M >= 0: with M = 0 dw and dbias are zeroed.  Outputs overlap nothing.
+ *   workspace  as for tbs_linear, from tbs_linear_backward_workspace with the same
+ *              activation and, as 0 or 1, which outputs are wanted.
+ * Errors as tbs_linear.
+ */
+size_t tbs_linear_backward_workspace(int32_t dtype, int32_t activation, int32_t M, int32_t N,
+                                     int32_t K, int32_t want_dx, int32_t want_dw,
+                                     int32_t want_dbias, int32_t want_dz);
+tbs_status tbs_linear_backward(int32_t dtype, const void *grad_out, int64_t ldg, const void *x,
+                               int64_t ldx, const void *w, int64_t ldw, const void *pre,
+                               int64_t ldp, int32_t activation, int32_t M, int32_t N,
+                               int32_t K, void *dx, int64_t lddx, void *dw, int64_t lddw,
+                               void *dbias, void *dz, int64_t lddz, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Logits (or log-probabilities, as tbs_joiner_logp gives them) adjusted before labels are
+ * taken from them.  For row r and label v of the vocabulary, in this order and in fp32:
+ *   where v occurs k > 0 times in the row's history,
+ *     z = (z > 0 ? z / repetition : z * repetition) - presence - frequency * k;
+ *   z += bias[v];
+ *   z = -inf where the row's bit mask has no bit v, or the row's state of the decoding
+ *     graph has no arc with label v (blank, 0, stays: it keeps the state);
+ *   normalize: z -= log sum over v of e^z.  A row whose masks leave nothing stays -inf
+ *     throughout; in one with a NaN or +inf left, whatever is not -inf becomes NaN.
+ *
+ *   dtype          element type of logits and out;
+ *   logits         DEVICE [R][V], rows of ld_logits elements; out likewise (ld_out), may be
+ *                  logits itself (same rows), overlaps nothing else; V >= 1;
+ *   history        DEVICE int32 [R][history_cols], rows of ld_history, or NULL: labels
+ *                  given so far; entries outside [0, V) count for nothing;
+ *   history_lengths DEVICE int32 [R] or NULL (all of history_cols): entries of each row
+ *                  that count, clamped to [0, history_cols];
+ *   repetition (finite, > 0), presence, frequency (finite): for every row, unless
+ *   row_penalties  DEVICE float [R][3] gives each row's own three (not checked);
+ *   bias           DEVICE float [R][V], rows of ld_bias (0: one row for all), or NULL;
+ *   allowed        DEVICE int32 [R][(V + 31) / 32], rows of ld_allowed words (0: one row
+ *                  for all), or NULL: bit v % 32 of word v / 32;
+ *   graph, states  a decoding graph of vocabulary V and DEVICE int32 [R], each row's state;
+ *                  a state outside the graph (-1, say) leaves its row without this mask.
+ *                  Both or neither NULL;
+ *   workspace      DEVICE, 16-byte aligned, of at least tbs_adjust_logits_workspace bytes
+ *                  (0: none, may be NULL); calls that may overlap need one each.
+ * R >= 0 (0 is a no-op).  Errors: TBS_EINVAL for an unknown dtype, sizes, NULL pointers, row
+ * lengths below the width, penalties out of range, a graph of another vocabulary or a
+ * workspace that is too small; TBS_ECAPACITY for R * V too large for a launch.
+ */
+typedef struct {
+  const int32_t *history;
+  int64_t ld_history;
+  int32_t history_cols;
+  const int32_t *history_lengths;
+  float repetition, presence, frequency;
+  const float *row_penalties;
+  const float *bias;
+  int64_t ld_bias;
+  const int32_t *allowed;
+  int64_t ld_allowed;
+  const tbs_graph *graph;
+  const int32_t *states;
+  int32_t normalize;
+} tbs_adjustments;
+
+size_t tbs_adjust_logits_workspace(int32_t dtype, int32_t R, int32_t V, int32_t normalize);
+tbs_status tbs_adjust_logits(int32_t dtype, const void *logits, int64_t ld_logits, int32_t R,
+                             int32_t V, const tbs_adjustments *adjustments, void *out,
+                             int64_t ld_out, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
 
 /*
  * How tbs_decode drives the frame loop of Algorithm 1 (all schedules compute

@@ -1899,4 +1899,285 @@ tbs_status tbs_transducer_forward(int32_t kind, const float* blank, const float*
   return TBS_OK;
 }
 
+namespace {
+
+// A caller's workspace of at least `need` bytes.
+tbs_status check_workspace(const char* who, const void* workspace, size_t bytes, size_t need) {
+  if (need == 0) return TBS_OK;
+  if (!workspace || bytes < need)
+    return fail(TBS_EINVAL, "%s: workspace of %zu bytes, needs %zu", who, workspace ? bytes : (size_t)0, need);
+  if ((uintptr_t)workspace % 16) return fail(TBS_EINVAL, "%s: workspace is not 16-byte aligned", who);
+  return TBS_OK;
+}
+
+bool known_dtype(int32_t dtype) { return dtype == kF32 || dtype == kBF16 || dtype == kF16; }
+size_t elem_size(int32_t dtype) { return dtype == kF32 ? 4 : 2; }
+size_t align16(size_t n) { return (n + 15) / 16 * 16; }
+
+tbs_status check_linear(const char* who, int32_t dtype, int32_t activation, int32_t M, int32_t N, int32_t K) {
+  if (!known_dtype(dtype)) return fail(TBS_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (activation < kActNone || activation > kActGelu)
+    return fail(TBS_EINVAL, "%s: unknown activation %d", who, activation);
+  if (M < 0 || N < 1 || K < 1) return fail(TBS_EINVAL, "%s: need M >= 0, N >= 1, K >= 1", who);
+  return TBS_OK;
+}
+
+tbs_status too_large(const char* who, int M, int N) {
+  return fail(TBS_ECAPACITY, "%s: a product of %d x %d results is too large for a launch", who, M, N);
+}
+
+// The three products of a linear layer, planned (pointers left out).
+bool plan_forward(ProductArgs& p, int32_t dtype, int32_t M, int32_t N, int32_t K) {
+  p = ProductArgs{};
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  return plan_product(p, dtype, true, true);
+}
+bool plan_dx(ProductArgs& p, int32_t dtype, int32_t M, int32_t N, int32_t K) {
+  p = ProductArgs{};
+  p.M = M;
+  p.N = K;
+  p.K = N;
+  return plan_product(p, dtype, true, false);
+}
+bool plan_dw(ProductArgs& p, int32_t dtype, int32_t M, int32_t N, int32_t K, bool dw, bool dbias) {
+  p = ProductArgs{};
+  p.M = N;
+  p.N = dw ? K : 1;  // dbias alone: one column of x, not stored
+  p.K = M;
+  p.rsum = dbias;
+  return plan_product(p, dtype, false, false);
+}
+void place_parts(ProductArgs& p, void* at) {
+  p.part = (float*)at;
+  p.rpart = p.part + (size_t)p.splits * p.M * p.N;
+}
+
+}  // namespace
+
+size_t tbs_transducer_gradient_workspace(int32_t B, int32_t T, int32_t U) {
+  if (B < 1 || T < 1 || U < 0) return 0;
+  return (transducer_cells(B, T, U) + B) * sizeof(int2);
+}
+
+tbs_status tbs_transducer_gradient(int32_t kind, const float* blank, const float* label,
+                                   const int32_t* lengths, const double* weights, int32_t B,
+                                   int32_t T, int32_t U, double* out_total,
+                                   float* out_grad_blank, float* out_grad_label,
+                                   int32_t* out_status, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream) {
+  const char* who = "tbs_transducer_gradient";
+  if (kind != TBS_TRANSDUCER_STANDARD && kind != TBS_TRANSDUCER_MODIFIED &&
+      kind != TBS_TRANSDUCER_CONSTRAINED)
+    return fail(TBS_EINVAL, "%s: unknown kind %d", who, (int)kind);
+  if (B < 0 || T < 1 || U < 0) return fail(TBS_EINVAL, "%s: need B >= 0, T >= 1, U >= 0", who);
+  if (U + 1 > 64 * kTransducerMaxK)
+    return fail(TBS_ECAPACITY, "%s: U = %d exceeds the limit %d", who, (int)U, 64 * kTransducerMaxK - 1);
+  if (B > 1 << 21) return fail(TBS_ECAPACITY, "%s: B = %d exceeds the limit %d", who, (int)B, 1 << 21);
+  if (B == 0) return TBS_OK;
+  if (!blank || (U > 0 && !label) || !lengths || !out_total || !out_grad_blank ||
+      (U > 0 && !out_grad_label))
+    return fail(TBS_EINVAL, "%s: NULL pointer", who);
+  const tbs_status s = check_workspace(who, workspace, workspace_bytes,
+                                       tbs_transducer_gradient_workspace(B, T, U));
+  if (s != TBS_OK) return s;
+  int2* cells = (int2*)workspace;
+  HIP_TRY(launch_transducer_gradient(kind, blank, label, lengths, weights, B, T, U, out_total,
+                                     out_grad_blank, out_grad_label, out_status, cells,
+                                     cells + transducer_cells(B, T, U), (hipStream_t)hip_stream),
+          "launch(transducer gradient)");
+  return TBS_OK;
+}
+
+size_t tbs_linear_workspace(int32_t dtype, int32_t M, int32_t N, int32_t K) {
+  if (!known_dtype(dtype) || M < 1 || N < 1 || K < 1) return 0;
+  ProductArgs p;
+  if (!plan_forward(p, dtype, M, N, K)) return 0;
+  return product_part_floats(p) * sizeof(float);
+}
+
+tbs_status tbs_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                      const void* bias, const void* residual, int64_t ldr,
+                      int32_t residual_after, int32_t activation, int32_t M, int32_t N,
+                      int32_t K, void* out, int64_t ldo, void* pre, int64_t ldp,
+                      void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const char* who = "tbs_linear";
+  tbs_status s = check_linear(who, dtype, activation, M, N, K);
+  if (s != TBS_OK) return s;
+  if (M == 0) return TBS_OK;
+  if (!x || !w || !out) return fail(TBS_EINVAL, "%s: NULL pointer", who);
+  if (ldx < K || ldw < K || ldo < N || (residual && ldr != 0 && ldr < N) || (pre && ldp < N))
+    return fail(TBS_EINVAL, "%s: a row length is below the width of its matrix", who);
+  ProductArgs p;
+  if (!plan_forward(p, dtype, M, N, K)) return too_large(who, M, N);
+  s = check_workspace(who, workspace, workspace_bytes, product_part_floats(p) * sizeof(float));
+  if (s != TBS_OK) return s;
+  p.a = x;
+  p.lda = ldx;
+  p.b = w;
+  p.ldb = ldw;
+  place_parts(p, workspace);
+  p.epi = LinearEpilogue{out, bias, residual, pre, ldo, ldr, ldp, activation, residual_after != 0};
+  HIP_TRY(launch_product(p, dtype, true, true, (hipStream_t)hip_stream), "launch(linear)");
+  return TBS_OK;
+}
+
+size_t tbs_linear_backward_workspace(int32_t dtype, int32_t activation, int32_t M, int32_t N,
+                                     int32_t K, int32_t want_dx, int32_t want_dw,
+                                     int32_t want_dbias, int32_t want_dz) {
+  if (!known_dtype(dtype) || M < 1 || N < 1 || K < 1) return 0;
+  ProductArgs p;
+  size_t parts = 0, dz = 0;
+  if (want_dx && plan_dx(p, dtype, M, N, K)) parts = product_part_floats(p);
+  if ((want_dw || want_dbias) && plan_dw(p, dtype, M, N, K, want_dw, want_dbias))
+    parts = std::max(parts, product_part_floats(p));
+  if (activation != kActNone && !want_dz && (want_dx || want_dw || want_dbias))
+    dz = align16((size_t)M * N * elem_size(dtype));
+  return dz + parts * sizeof(float);  // (the products take turns at the parts)
+}
+
+tbs_status tbs_linear_backward(int32_t dtype, const void* grad_out, int64_t ldg, const void* x,
+                               int64_t ldx, const void* w, int64_t ldw, const void* pre,
+                               int64_t ldp, int32_t activation, int32_t M, int32_t N,
+                               int32_t K, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                               void* dbias, void* dz, int64_t lddz, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  const char* who = "tbs_linear_backward";
+  tbs_status s = check_linear(who, dtype, activation, M, N, K);
+  if (s != TBS_OK) return s;
+  if (!dx && !dw && !dbias && !dz) return TBS_OK;
+  const bool act = activation != kActNone, products = dx || dw || dbias;
+  if (M > 0 && (!grad_out || (act && !pre) || (dx && !w) || (dw && !x)))
+    return fail(TBS_EINVAL, "%s: NULL pointer", who);
+  if ((M > 0 && (ldg < N || (act && ldp < N) || (dx && ldw < K) || (dw && ldx < K))) ||
+      (dx && lddx < K) || (dw && lddw < K) || (act && dz && lddz < N))
+    return fail(TBS_EINVAL, "%s: a row length is below the width of its matrix", who);
+  ProductArgs pdx, pdw;
+  if (dx && M > 0 && !plan_dx(pdx, dtype, M, N, K)) return too_large(who, M, K);
+  if ((dw || dbias) && !plan_dw(pdw, dtype, M, N, K, dw, dbias)) return too_large(who, N, K);
+  s = check_workspace(who, workspace, workspace_bytes,
+                      tbs_linear_backward_workspace(dtype, activation, M, N, K, dx != nullptr,
+                                                    dw != nullptr, dbias != nullptr, dz != nullptr));
+  if (s != TBS_OK) return s;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char* parts = (char*)workspace;
+  const void* g = grad_out;
+  long long ld = ldg;
+  if (act && M > 0 && (products || dz)) {
+    void* to = dz;
+    long long ldt = lddz;
+    if (!dz) {
+      to = workspace;
+      ldt = N;
+      parts += align16((size_t)M * N * elem_size(dtype));
+    }
+    HIP_TRY(launch_act_grad(dtype, grad_out, ldg, pre, ldp, to, ldt, M, N, activation, st),
+            "launch(activation gradient)");
+    g = to;
+    ld = ldt;
+  }
+  if (dx && M > 0) {
+    pdx.a = g;
+    pdx.lda = ld;
+    pdx.b = w;
+    pdx.ldb = ldw;
+    place_parts(pdx, parts);
+    pdx.epi = LinearEpilogue{dx, nullptr, nullptr, nullptr, lddx, 0, 0, kActNone, 0};
+    HIP_TRY(launch_product(pdx, dtype, true, false, st), "launch(linear dx)");
+  }
+  if (dw || dbias) {
+    pdw.a = g;
+    pdw.lda = ld;
+    pdw.b = dw ? x : g;  // dbias alone: any operand will do
+    pdw.ldb = dw ? ldx : ld;
+    pdw.rout = dbias;
+    place_parts(pdw, parts);
+    pdw.epi = LinearEpilogue{dw, nullptr, nullptr, nullptr, lddw, 0, 0, kActNone, 0};
+    HIP_TRY(launch_product(pdw, dtype, false, false, st), "launch(linear dw)");
+  }
+  return TBS_OK;
+}
+
+namespace {
+
+tbs_status plan_adjust_logits(AdjustArgs& p, int32_t dtype, int32_t R, int32_t V, int32_t normalize) {
+  p = AdjustArgs{};
+  p.R = R;
+  p.V = V;
+  p.normalize = normalize != 0;
+  if (!plan_adjust(p, dtype))
+    return fail(TBS_ECAPACITY, "tbs_adjust_logits: %d rows of %d labels are too many for a launch", R, V);
+  return TBS_OK;
+}
+
+}  // namespace
+
+size_t tbs_adjust_logits_workspace(int32_t dtype, int32_t R, int32_t V, int32_t normalize) {
+  if (!known_dtype(dtype) || R < 1 || V < 1) return 0;
+  AdjustArgs p;
+  if (plan_adjust_logits(p, dtype, R, V, normalize) != TBS_OK) return 0;
+  return adjust_workspace(p);
+}
+
+tbs_status tbs_adjust_logits(int32_t dtype, const void* logits, int64_t ld_logits, int32_t R,
+                             int32_t V, const tbs_adjustments* adjustments, void* out,
+                             int64_t ld_out, void* workspace, size_t workspace_bytes,
+                             void* hip_stream) {
+  const char* who = "tbs_adjust_logits";
+  if (!known_dtype(dtype)) return fail(TBS_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (R < 0 || V < 1) return fail(TBS_EINVAL, "%s: need R >= 0, V >= 1", who);
+  if (!adjustments) return fail(TBS_EINVAL, "%s: adjustments is NULL", who);
+  const tbs_adjustments& a = *adjustments;
+  if (a.history && (a.history_cols < 0 || a.ld_history < a.history_cols))
+    return fail(TBS_EINVAL, "%s: history_cols %d, ld_history %lld", who, a.history_cols,
+                (long long)a.ld_history);
+  if (!(a.repetition > 0.f) || !std::isfinite(a.repetition) || !std::isfinite(a.presence) ||
+      !std::isfinite(a.frequency))
+    return fail(TBS_EINVAL, "%s: penalties must be finite, repetition > 0", who);
+  if ((a.graph != nullptr) != (a.states != nullptr))
+    return fail(TBS_EINVAL, "%s: graph and states go together", who);
+  if (a.graph && a.graph->V != V)
+    return fail(TBS_EINVAL, "%s: graph vocab_size %d != %d", who, a.graph->V, V);
+  if ((a.bias && a.ld_bias != 0 && a.ld_bias < V) ||
+      (a.allowed && a.ld_allowed != 0 && a.ld_allowed < (V + 31) / 32))
+    return fail(TBS_EINVAL, "%s: a row length is below the width of its matrix", who);
+  if (R == 0) return TBS_OK;
+  if (!logits || !out) return fail(TBS_EINVAL, "%s: NULL pointer", who);
+  if (ld_logits < V || ld_out < V)
+    return fail(TBS_EINVAL, "%s: a row length is below the width of its matrix", who);
+  AdjustArgs p;
+  tbs_status s = plan_adjust_logits(p, dtype, R, V, a.normalize);
+  if (s != TBS_OK) return s;
+  s = check_workspace(who, workspace, workspace_bytes, adjust_workspace(p));
+  if (s != TBS_OK) return s;
+  p.logits = logits;
+  p.out = out;
+  p.ldz = ld_logits;
+  p.ldo = ld_out;
+  if (a.history && a.history_cols > 0) {
+    p.history = a.history;
+    p.ldh = a.ld_history;
+    p.L = a.history_cols;
+    p.hlen = a.history_lengths;
+    p.row_penalties = a.row_penalties;
+  }
+  p.repetition = a.repetition;
+  p.presence = a.presence;
+  p.frequency = a.frequency;
+  p.bias = a.bias;
+  p.ldb = a.ld_bias;
+  p.allowed = (const uint32_t*)a.allowed;
+  p.ldm = a.ld_allowed;
+  if (a.graph && !a.graph->trivial) {  // (a trivial graph allows every label)
+    p.graph_rp = a.graph->rp;
+    p.graph_label = a.graph->label;
+    p.S = a.graph->S;
+    p.states = a.states;
+  }
+  p.stats = (float2*)workspace;
+  HIP_TRY(launch_adjust(p, dtype, (hipStream_t)hip_stream), "launch(adjust logits)");
+  return TBS_OK;
+}
+
 }  // extern "C"

@@ -340,4 +340,82 @@ hipError_t launch_transducer_forward(int kind, const float* blank, const float* 
                                      const int* lengths, int B, int T, int U, double* total,
                                      float* alpha, int* status, hipStream_t st);
 
+// Gradient of the transducer losses with respect to the inputs: weights[b] d total[b].
+// cells: workspace of transducer_cells(B, T, U) entries; zcell: [B].
+inline size_t transducer_cells(int B, int T, int U) { return (size_t)2 * B * T * (U + 1); }
+hipError_t launch_transducer_gradient(int kind, const float* blank, const float* label, const int* lengths,
+                                      const double* weights, int B, int T, int U, double* total,
+                                      float* grad_blank, float* grad_label, int* status, int2* cells,
+                                      int2* zcell, hipStream_t st);
+
+// Element types and activations of the linear layers and adjusted logits (tbs_dtype,
+// tbs_activation).
+constexpr int kF32 = 0, kBF16 = 1, kF16 = 2;
+constexpr int kActNone = 0, kActRelu = 1, kActTanh = 2, kActSilu = 3, kActGelu = 4;
+
+// out = act(z + bias + res), or act(z + bias) + res; pre: the activation's argument.  Rows of
+// ld elements; bias, res and pre may be null.
+struct LinearEpilogue {
+  void* out;
+  const void* bias;
+  const void* res;
+  void* pre;
+  long long ldo, ldr, ldp;
+  int act, res_after;
+};
+
+// C[m][n] = sum_k A(m, k) B(n, k), m < M, n < N, k < K (linear.hip).
+struct ProductArgs {
+  const void* a;            // rows of lda elements: of k for each m, or of m for each k
+  const void* b;            // rows of ldb elements: of k for each n, or of n for each k
+  long long lda, ldb;
+  int M, N, K;
+  int shape;                // tile (plan_product)
+  int tiles_m, tiles_n;
+  int splits, slices_per;   // parts of k, and slices of k in each
+  float* part;              // [splits][M][N] partial sums (splits > 1)
+  int rsum;                 // the sums of A's rows too, to rout [M]
+  float* rpart;             // [splits][M] (splits > 1)
+  void* rout;
+  LinearEpilogue epi;
+};
+// Chooses tile and split of a product; false if it has too many tiles for a launch.
+bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc);
+inline size_t product_part_floats(const ProductArgs& p) {
+  return p.splits > 1 ? (size_t)p.splits * p.M * ((size_t)p.N + (p.rsum ? 1 : 0)) : 0;
+}
+hipError_t launch_product(const ProductArgs& p, int dtype, bool akc, bool bkc, hipStream_t st);
+hipError_t launch_act_grad(int dtype, const void* dy, long long ldy, const void* pre, long long ldp, void* dz,
+                           long long ldz, int M, int N, int act, hipStream_t st);
+
+// Adjusted logits (adjust.hip).
+struct AdjustArgs {
+  const void* logits;       // [R] rows of ldz elements
+  void* out;                // [R] rows of ldo elements
+  long long ldz, ldo;
+  int R, V;
+  const int* history;       // [R] rows of ldh labels, or null
+  long long ldh;
+  int L;
+  const int* hlen;          // [R], or null: L each
+  float repetition, presence, frequency;
+  const float* row_penalties;  // [R][3], or null
+  const float* bias;        // [R] rows of ldb, or null
+  long long ldb;
+  const uint32_t* allowed;  // [R] rows of ldm words, or null
+  long long ldm;
+  const int* graph_rp;      // arcs of the rows' states, or null
+  const int* graph_label;
+  int S;
+  const int* states;        // [R]
+  int normalize;
+  float2* stats;            // workspace [R][parts] (parts > 1)
+  int parts, per;           // workgroups per row and columns of each
+};
+bool plan_adjust(AdjustArgs& p, int dtype);
+inline size_t adjust_workspace(const AdjustArgs& p) {
+  return p.parts > 1 && p.normalize ? (size_t)p.R * p.parts * sizeof(float2) : 0;
+}
+hipError_t launch_adjust(const AdjustArgs& p, int dtype, hipStream_t st);
+
 }  // namespace tbs

@@ -13,6 +13,7 @@
 //    [kRingMinLog, kRingMaxLog].
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "internal.h"
@@ -625,7 +626,213 @@ hipError_t launch_kind(const RingPlan& p, const float* blank, const float* label
   }
 }
 
+// ---------------------------------------------------------------------------
+// Gradient.  With alpha(t, u) the weight of the paths into a cell and beta(t, u) of those
+// from it to the end (as sums of products), Z the likelihood, pb = e^blank and pl = e^label,
+// d log Z / d input is the share of the paths that use the input:
+//   eq. (1)  blank(t, u): alpha(t, u) pb(t, u) beta(t+1, u) / Z (1 at the last cell),
+//            label(t, u): alpha(t, u) pl(t, u) beta(t, u+1) / Z;
+//   eq. (2)  label(t, u): alpha(t, u) pl(t, u) beta(t+1, u+1) / Z, blank as in eq. (1);
+//   eq. (3)  with g(t, u) = pb(t, u) beta(t+1, u), the weight of what follows an arrival on
+//            context u in frame t: label(t, u): alpha(t, u) pl(t, u) g(t, u+1) / Z,
+//            blank(t, u): (alpha(t, u) + pl(t, u-1) alpha(t, u-1)) g(t, u) / Z.
+// beta (and g) obey alpha's recursion with frames and labels counted from the end: with
+// j = U_b - u, step row i (see the ring) takes label row T_b - 1 - i and blank row T_b - 1 - i
+// (eq. 1, 2; for eq. (1) the cell's own, its last blank left out as a factor of all) or
+// T_b - 2 - i (eq. 3, whose last blank is a factor too).  So one kernel computes both, a
+// workgroup per utterance and direction, and a second one the shares.  A score is kept as
+// m 2^e (m a float in [0.5, 1]), so that shares lose nothing to the size of the scores.
+
+constexpr float kLn2Lo = 1.42860677e-6f;  // ln 2 = kLn2Hi + kLn2Lo, kLn2Hi with 16 bits
+constexpr float kLn2Hi = 0.69314575f;
+
+__device__ __forceinline__ bool reachable(int2 c) { return c.y > kZeroExp / 2; }
+__device__ __forceinline__ int2 zero_cell() { return make_int2(__float_as_int(0.5f), kZeroExp); }
+// e^v; below 2^(kZeroExp / 2) it counts as 0, above 2^(-kZeroExp / 2) as infinite
+__device__ __forceinline__ int2 log_to_cell(double v) {
+  const double t = v * 1.4426950408889634;
+  if (t <= (double)(kZeroExp / 2)) return zero_cell();
+  if (!(t < (double)(-kZeroExp / 2))) return make_int2(__float_as_int(v == v ? INFINITY : NAN), 0);
+  const double e = floor(t) + 1.0;
+  return make_int2(__float_as_int((float)exp2(t - e)), (int)e);
+}
+
+// Rows of an utterance's inputs that step row i reads, in either direction (row of blank,
+// row of label; -1: none, the input counts as probability 1 or leads nowhere).
+template <int KIND, bool REV>
+__device__ __forceinline__ int blank_row(int i, int Tb) {
+  if (!REV) return KIND == 0 ? i - 1 : i;
+  return KIND == 2 ? Tb - 2 - i : Tb - 1 - i;
+}
+
+// Log-domain scores of one utterance and direction: cells [T][U + 1] of this direction,
+// state before step row i (eq. 2, 3) or of row i (eq. 1) at row i.
+template <int KIND, bool REV>
+__device__ void log_scores(const float* __restrict__ bl, const float* __restrict__ lb, int Tb, int Ub, int U,
+                           int2* __restrict__ cells, double* buf, double* __restrict__ total,
+                           int2* __restrict__ zcell) {
+  const LogAdd log_add;
+  const int tid = threadIdx.x, U1 = U + 1;
+  for (int u = tid; u <= Ub; u += kRingThreads) buf[u] = u == 0 ? 0.0 : ninf();
+  __syncthreads();
+  const int steps = Tb + (KIND == 0 ? Ub : 0);
+  for (int s = 0; s < steps; ++s) {
+    const double* prev = buf + (s & 1) * U1;
+    double* next = buf + (~s & 1) * U1;
+    for (int u = tid; u <= Ub; u += kRingThreads) {
+      const int i = KIND == 0 ? s - u : s;
+      double v = prev[u];
+      if (i >= 0 && i < Tb) {
+        if (KIND != 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
+        const int rb = blank_row<KIND, REV>(i, Tb), rl = REV ? Tb - 1 - i : i;
+        const bool use = KIND == 0 ? i > 0 : rb >= 0;
+        const double xb = use ? (double)bl[(size_t)rb * U1 + (REV ? Ub - u : u)] : 0.0;
+        double w = ninf();
+        if (u > 0) {
+          w = prev[u - 1] + (double)lb[(size_t)rl * U + (REV ? Ub - u : u - 1)];
+          if (KIND == 2) w += xb;
+        }
+        v = KIND == 0 && i == 0 ? (u == 0 ? 0.0 : ninf()) : v + xb;
+        v = log_add(v, w);
+        if (KIND == 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
+      }
+      next[u] = v;
+    }
+    __syncthreads();
+  }
+  if (!REV && tid == 0) {
+    double res = buf[(steps & 1) * U1 + Ub];
+    int2 z = log_to_cell(res);
+    if (KIND == 0) {  // the last blank is left out of z, unless it settles the matter
+      res += (double)bl[(size_t)(Tb - 1) * U1 + Ub];
+      const int2 all = log_to_cell(res);
+      if (!reachable(all) || !(__int_as_float(all.x) < INFINITY)) z = all;
+    }
+    *zcell = z;
+    *total = res;
+  }
+}
+
+template <int KIND>
+__global__ __launch_bounds__(kRingThreads) void k_scores_logs(
+    const float* __restrict__ blank, const float* __restrict__ label, const int* __restrict__ lengths, int T,
+    int U, double* __restrict__ total, int* __restrict__ status, int2* __restrict__ cells,
+    int2* __restrict__ zcell) {
+  __shared__ double buf[2 * 64 * kTransducerMaxK];
+  const int b = blockIdx.x >> 1, rev = blockIdx.x & 1;
+  int Tb, Ub;
+  if (!utterance(lengths, b, T, U, total, status, threadIdx.x == 0 && !rev, Tb, Ub)) return;
+  if (threadIdx.x == 0 && !rev && status) status[b] = 0;
+  const float* bl = blank + (size_t)b * T * (U + 1);
+  const float* lb = label + (size_t)b * T * U;
+  int2* c = cells + ((size_t)2 * b + rev) * T * (U + 1);
+  if (rev) log_scores<KIND, true>(bl, lb, Tb, Ub, U, c, buf, total + b, zcell + b);
+  else log_scores<KIND, false>(bl, lb, Tb, Ub, U, c, buf, total + b, zcell + b);
+}
+
+// e^x = (what is returned) 2^k
+__device__ __forceinline__ float exp_parts(float x, int& k) {
+  const float xc = fminf(fmaxf(x, -1e8f), 1e8f);  // (beyond it what it leads to is 0 or infinite)
+  const float r = rintf(xc * 1.44269504f);
+  k = (int)r;
+  return __expf(__builtin_fmaf(-r, kLn2Lo, __builtin_fmaf(-r, kLn2Hi, x == x ? xc : x)));
+}
+// a e^x b / z for cells a and b (0 if one is unreachable or x is -inf); rz: 1 / z's mantissa
+__device__ __forceinline__ float share(int2 a, float x, int2 b, float rz, int ez) {
+  if (!reachable(a) || !reachable(b) || x == -INFINITY) return 0.f;
+  int k;
+  const float m = exp_parts(x, k) * __int_as_float(a.x) * __int_as_float(b.x) * rz;
+  const long long e = (long long)a.y + b.y - ez + k;
+  return ldexpf(m, (int)(e < -400 ? -400 : e > 400 ? 400 : e));
+}
+
+constexpr int kShareCells = 1024;  // cells per workgroup and turn
+
+template <int KIND>
+__global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank, const float* __restrict__ label,
+                                                const int* __restrict__ lengths,
+                                                const double* __restrict__ weights, int T, int U, int parts,
+                                                const int2* __restrict__ cells, const int2* __restrict__ zcell,
+                                                float* __restrict__ grad_blank, float* __restrict__ grad_label) {
+  const int b = blockIdx.x / parts, part = blockIdx.x % parts, U1 = U + 1;
+  const long long n = (long long)T * U1;
+  const int Tb = lengths[2 * b], Ub = lengths[2 * b + 1];
+  const bool ok = Tb >= 1 && Tb <= T && Ub >= 0 && Ub <= U;
+  const int2 zc = ok ? zcell[b] : zero_cell();
+  const bool live = ok && reachable(zc);
+  const float zm = __int_as_float(zc.x);
+  const bool bad = !(zm < INFINITY);
+  float rz = 1.f / zm;
+  int ez = zc.y;
+  const double w = weights ? weights[b] : 1.0;
+  const int2* ca = cells + (size_t)2 * b * n;
+  const int2* cb = ca + n;
+  const float* bl = blank + (size_t)b * n;
+  const float* lb = label + (size_t)b * T * U;
+  float* gb = grad_blank + (size_t)b * n;
+  float* gl = grad_label + (size_t)b * T * U;
+  if (KIND == 2 && live) {  // the last blank, a factor of g
+    int k;
+    rz *= exp_parts(bl[(size_t)(Tb - 1) * U1 + Ub], k);
+    ez -= k;
+  }
+  for (long long at = (long long)part * kShareCells + threadIdx.x; at < n; at += 256) {
+    const int t = (int)(at / U1), u = (int)(at - (long long)t * U1);
+    float sb = 0.f, sl = 0.f;
+    if (live && t < Tb && u <= Ub) {
+      const int2 a = ca[at];
+      const int2* row = cb + (size_t)(Tb - 1 - t) * U1 + (Ub - u);  // the same frame and label
+      const bool lab = u < Ub;
+      const float xl = lab ? lb[(size_t)t * U + u] : 0.f;
+      if (KIND == 0) {
+        const bool last = t == Tb - 1;
+        if (last) sb = u == Ub ? 1.f : 0.f;
+        else sb = share(a, bl[at], row[-(ptrdiff_t)U1], rz, ez);
+      } else if (KIND == 1) {
+        sb = share(a, bl[at], row[0], rz, ez);
+      } else {
+        sb = share(a, 0.f, row[0], rz, ez);
+        if (u > 0) sb += share(ca[at - 1], lb[(size_t)t * U + u - 1], row[0], rz, ez);
+      }
+      if (lab) sl = share(a, xl, row[-1], rz, ez);
+      if (bad) sb = sl = NAN;
+      sb = (float)(w * (double)sb);
+      sl = (float)(w * (double)sl);
+    }
+    gb[at] = sb;
+    if (u < U) gl[(size_t)t * U + u] = sl;
+    if (((at + 256) & ~(long long)(kShareCells - 1)) != (at & ~(long long)(kShareCells - 1)))
+      at += (long long)(parts - 1) * kShareCells;
+  }
+}
+
+template <int KIND>
+hipError_t launch_gradient(const float* blank, const float* label, const int* lengths, const double* weights, int B,
+                           int T, int U, double* total, float* grad_blank, float* grad_label, int* status,
+                           int2* cells, int2* zcell, hipStream_t st) {
+  hipLaunchKernelGGL(k_scores_logs<KIND>, dim3(2 * B), dim3(kRingThreads), 0, st, blank, label, lengths, T, U,
+                     total, status, cells, zcell);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long long n = (long long)T * (U + 1);
+  const long long want = (n + kShareCells - 1) / kShareCells, most = std::max(1, (1 << 22) / B);
+  const int parts = (int)std::min(want, most);
+  hipLaunchKernelGGL(k_shares<KIND>, dim3(B * parts), dim3(256), 0, st, blank, label, lengths, weights, T, U, parts,
+                     cells, zcell, grad_blank, grad_label);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_transducer_gradient(int kind, const float* blank, const float* label, const int* lengths,
+                                      const double* weights, int B, int T, int U, double* total,
+                                      float* grad_blank, float* grad_label, int* status, int2* cells,
+                                      int2* zcell, hipStream_t st) {
+  if (B == 0) return hipSuccess;
+  if (U + 1 > 64 * kTransducerMaxK) return hipErrorInvalidValue;
+  auto* fn = kind == 0 ? launch_gradient<0> : kind == 1 ? launch_gradient<1> : launch_gradient<2>;
+  return fn(blank, label, lengths, weights, B, T, U, total, grad_blank, grad_label, status, cells, zcell, st);
+}
 
 hipError_t launch_transducer_forward(int kind, const float* blank, const float* label,
                                      const int* lengths, int B, int T, int U, double* total,

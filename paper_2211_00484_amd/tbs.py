@@ -7,6 +7,7 @@ the first call does, and raises if ``libtbs.so`` has not been built.
 from __future__ import annotations
 
 import atexit
+import contextlib
 import ctypes
 import math
 import os
@@ -27,6 +28,9 @@ STATUS_NAMES = {0: "TBS_OK", -1: "TBS_EINVAL", -2: "TBS_ENOMEM", -3: "TBS_EDEVIC
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
+_SZ = ctypes.c_size_t
+_F32 = ctypes.c_float
 
 
 class TbsError(RuntimeError):
@@ -46,6 +50,14 @@ SCHEDULES = {"auto": 0, "frame": 1, "stream": 2, "stream1": 3}
 class BeamParams(ctypes.Structure):
     _fields_ = [("beam", ctypes.c_float), ("max_states", ctypes.c_int32),
                 ("max_contexts", ctypes.c_int32)]
+
+
+class Adjustments(ctypes.Structure):
+    _fields_ = [("history", _P), ("ld_history", _I64), ("history_cols", _I32),
+                ("history_lengths", _P), ("repetition", _F32), ("presence", _F32),
+                ("frequency", _F32), ("row_penalties", _P), ("bias", _P), ("ld_bias", _I64),
+                ("allowed", _P), ("ld_allowed", _I64), ("graph", _P), ("states", _P),
+                ("normalize", _I32)]
 
 
 _lib = None
@@ -134,6 +146,26 @@ def lib():
                                           ctypes.POINTER(_P)]
     L.tbs_transducer_forward.restype = _I32
     L.tbs_transducer_forward.argtypes = [_I32, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P]
+    L.tbs_transducer_gradient_workspace.restype = _SZ
+    L.tbs_transducer_gradient_workspace.argtypes = [_I32] * 3
+    L.tbs_transducer_gradient.restype = _I32
+    L.tbs_transducer_gradient.argtypes = [_I32, _P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P,
+                                          _P, _SZ, _P]
+    L.tbs_linear_workspace.restype = _SZ
+    L.tbs_linear_workspace.argtypes = [_I32] * 4
+    L.tbs_linear.restype = _I32
+    L.tbs_linear.argtypes = [_I32, _P, _I64, _P, _I64, _P, _P, _I64, _I32, _I32, _I32, _I32, _I32,
+                             _P, _I64, _P, _I64, _P, _SZ, _P]
+    L.tbs_linear_backward_workspace.restype = _SZ
+    L.tbs_linear_backward_workspace.argtypes = [_I32] * 9
+    L.tbs_linear_backward.restype = _I32
+    L.tbs_linear_backward.argtypes = [_I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _I32,
+                                      _I32, _I32, _P, _I64, _P, _I64, _P, _P, _I64, _P, _SZ, _P]
+    L.tbs_adjust_logits_workspace.restype = _SZ
+    L.tbs_adjust_logits_workspace.argtypes = [_I32] * 4
+    L.tbs_adjust_logits.restype = _I32
+    L.tbs_adjust_logits.argtypes = [_I32, _P, _I64, _I32, _I32, ctypes.POINTER(Adjustments), _P,
+                                    _I64, _P, _SZ, _P]
     L.tbs_hyp_search.restype = _I32
     L.tbs_hyp_search.argtypes = [_P, ctypes.POINTER(HypParams), _P, _P, _I32, _I32, _P, _P, _P,
                                  _P, _P]
@@ -608,3 +640,258 @@ def transducer_forward(kind: str, blank, label, lengths, want_alpha: bool = Fals
                                         _dev_ptr(lengths), B, T, U, _dev_ptr(total),
                                         _dev_ptr(alpha), _dev_ptr(status), _stream_ptr(stream)))
     return total, alpha, status
+
+
+# Element types by the names torch gives them.
+_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "tanh": 2, "silu": 3, "gelu": 4}
+_I32_MAX = 2 ** 31 - 1
+
+
+def _scope(t, stream):
+    """Context in which the copies, outputs and workspace of a call on tensor ``t`` are
+    allocated and its kernels launched: the given stream, or the current stream of the
+    tensor's device."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+        return torch.cuda.stream(stream)
+    if t.device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(t.device)
+
+
+def _dtype_code(t) -> int:
+    code = _DTYPES.get(str(t.dtype))
+    if code is None:
+        raise ValueError(f"unsupported dtype {t.dtype}: float32, bfloat16 or float16")
+    return code
+
+
+def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False):
+    """(2-D tensor, row length) of ``t`` [..., cols]: a view where its rows are contiguous
+    and no closer than their width, else a copy.  With one_row, a [cols] or [1, cols] tensor
+    stands for all rows (row length 0)."""
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name} must be {dtype or like.dtype}, not {t.dtype}")
+    if t.dim() == 0 or t.shape[-1] != cols:
+        raise ValueError(f"{name} must have {cols} columns, not shape {tuple(t.shape)}")
+    m = t if t.dim() == 2 else t.reshape(-1, cols)
+    n = m.shape[0]
+    if rows is not None and n != rows and not (one_row and n == 1):
+        raise ValueError(f"{name} must have {rows} rows, not {n}")
+    if cols > 1 and m.stride(1) != 1:
+        m = m.contiguous()
+    if one_row and (n == 1 or m.stride(0) == 0):
+        return m, 0
+    if n > 1 and m.stride(0) < cols:
+        m = m.contiguous()
+    return m, m.stride(0) if n > 1 else cols
+
+
+def _vector(t, like, n: int, name: str, dtype=None):
+    if t.device != like.device or t.dtype != (dtype or like.dtype) or tuple(t.shape) != (n,):
+        raise ValueError(f"{name} must be {dtype or like.dtype} [{n}] on {like.device}, not "
+                         f"{t.dtype} {list(t.shape)} on {t.device}")
+    return t.contiguous()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(nbytes: int, like):
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def _rows32(n: int, name: str) -> int:
+    if n > _I32_MAX:
+        raise ValueError(f"{name}: {n} rows, at most {_I32_MAX}")
+    return n
+
+
+def linear(x, weight, bias=None, residual=None, activation: str = "none",
+           residual_after: bool = False, want_pre: bool = False, stream=None):
+    """act(x weight^T + bias + residual), or act(x weight^T + bias) + residual with
+    residual_after (tbs_linear): x [..., K], weight [N, K], bias [N], residual [..., N] or one
+    row [N] for all, of one dtype (float32, bfloat16, float16); sums in fp32.  activation:
+    "none", "relu", "tanh", "silu" or "gelu" (by erf).  Returns out [..., N], or (out, pre)
+    with want_pre: the activation's argument, for linear_backward.  Tensors whose rows are
+    not contiguous are copied; autograd does not see the call."""
+    import torch
+    with _scope(x, stream):
+        code, act = _dtype_code(x), ACTIVATIONS[activation]
+        if x.dim() == 0 or weight.dim() != 2:
+            raise ValueError("x must be [..., K] and weight [N, K]")
+        N, K = (int(n) for n in weight.shape)
+        x2, ldx = _matrix(x, x, K, "x")
+        M = _rows32(int(x2.shape[0]), "x")
+        w2, ldw = _matrix(weight, x, K, "weight")
+        b = None if bias is None else _vector(bias, x, N, "bias")
+        r, ldr = (None, 0) if residual is None else _matrix(residual, x, N, "residual", rows=M,
+                                                            one_row=True)
+        out = torch.empty(x.shape[:-1] + (N,), dtype=x.dtype, device=x.device)
+        pre = torch.empty_like(out) if want_pre else None
+        L = lib()
+        nbytes = L.tbs_linear_workspace(code, M, N, K)
+        ws = _workspace(nbytes, x)
+        _check(L.tbs_linear(code, _ptr(x2), ldx, _ptr(w2), ldw, _ptr(b), _ptr(r), ldr,
+                            int(residual_after), act, M, N, K, _ptr(out), N, _ptr(pre), N,
+                            _ptr(ws), nbytes, _stream_ptr()))
+    return (out, pre) if want_pre else out
+
+
+@dataclass
+class LinearGrads:
+    x: "object"       # [..., K] or None
+    weight: "object"  # [N, K] or None
+    bias: "object"    # [N] or None
+    pre: "object"     # [..., N] or None: of the activation's argument (and so of a residual
+                      # added before it); a residual added after it has grad_out's
+
+
+def linear_backward(grad_out, x, weight, pre=None, activation: str = "none",
+                    want_x: bool = True, want_weight: bool = True, want_bias: bool = True,
+                    want_pre: bool = False, stream=None) -> LinearGrads:
+    """Gradients of ``linear`` (tbs_linear_backward) from grad_out [..., N], its x and weight,
+    and, unless the activation is "none", the pre it returned."""
+    import torch
+    with _scope(grad_out, stream):
+        code, act = _dtype_code(grad_out), ACTIVATIONS[activation]
+        if x.dim() == 0 or weight.dim() != 2 or grad_out.dim() == 0:
+            raise ValueError("grad_out must be [..., N], x [..., K] and weight [N, K]")
+        N, K = (int(n) for n in weight.shape)
+        if grad_out.shape[:-1] != x.shape[:-1]:
+            raise ValueError("grad_out and x differ in their leading dimensions")
+        if (act != 0) != (pre is not None):
+            raise ValueError("pre goes with an activation, and only with one")
+        g, ldg = _matrix(grad_out, grad_out, N, "grad_out")
+        M = _rows32(int(g.shape[0]), "grad_out")
+        x2, ldx = _matrix(x, grad_out, K, "x", rows=M)
+        w2, ldw = _matrix(weight, grad_out, K, "weight")
+        p, ldp = (None, 0) if pre is None else _matrix(pre, grad_out, N, "pre", rows=M)
+        like = dict(dtype=grad_out.dtype, device=grad_out.device)
+        dx = torch.empty(x.shape, **like) if want_x else None
+        dw = torch.empty((N, K), **like) if want_weight else None
+        db = torch.empty(N, **like) if want_bias else None
+        dz = torch.empty(grad_out.shape, **like) if want_pre and act else None
+        L = lib()
+        nbytes = L.tbs_linear_backward_workspace(code, act, M, N, K, int(want_x),
+                                                 int(want_weight), int(want_bias),
+                                                 int(dz is not None))
+        ws = _workspace(nbytes, grad_out)
+        _check(L.tbs_linear_backward(code, _ptr(g), ldg, _ptr(x2), ldx, _ptr(w2), ldw, _ptr(p),
+                                     ldp, act, M, N, K, _ptr(dx), K, _ptr(dw), K, _ptr(db),
+                                     _ptr(dz), N, _ptr(ws), nbytes, _stream_ptr()))
+    return LinearGrads(x=dx, weight=dw, bias=db,
+                       pre=(dz if act else grad_out) if want_pre else None)
+
+
+def adjust_logits(logits, history=None, history_lengths=None, repetition: float = 1.0,
+                  presence: float = 0.0, frequency: float = 0.0, row_penalties=None, bias=None,
+                  allowed=None, graph: Optional[Graph] = None, states=None,
+                  normalize: bool = False, out=None, stream=None):
+    """Logits [..., V] with penalties for the labels of each row's history, biases, masks
+    and, with normalize, their log-softmax (tbs_adjust_logits); float32, bfloat16 or float16.
+    history int32 [R, L] (entries outside [0, V), such as -1 padding, do not count),
+    history_lengths int32 [R]; row_penalties float32 [R, 3] (repetition, presence, frequency)
+    in place of the three numbers; bias float32 [V] or [R, V]; allowed int32 [W] or [R, W],
+    W = (V + 31) // 32: bit v % 32 of word v // 32 allows label v; graph and states int32
+    [R]: only blank and the labels on arcs out of each row's state (-1: no such mask).
+    out: a tensor like logits, or logits itself."""
+    import torch
+    with _scope(logits, stream):
+        code = _dtype_code(logits)
+        if logits.dim() == 0 or logits.shape[-1] == 0:
+            raise ValueError("logits must be [..., V]")
+        V, i32 = int(logits.shape[-1]), torch.int32
+        z, ldz = _matrix(logits, logits, V, "logits")
+        R = _rows32(int(z.shape[0]), "logits")
+        if (graph is None) != (states is None):
+            raise ValueError("graph and states go together")
+        a = Adjustments(repetition=float(repetition), presence=float(presence),
+                        frequency=float(frequency), normalize=int(bool(normalize)))
+        keep = []
+        if history is not None:
+            if history.dim() != 2:
+                raise ValueError("history must be [R, L]")
+            h, ldh = _matrix(history, logits, int(history.shape[1]), "history", i32, rows=R)
+            a.history, a.ld_history, a.history_cols = _ptr(h), ldh, int(h.shape[1])
+            keep.append(h)
+        elif history_lengths is not None or row_penalties is not None:
+            raise ValueError("history_lengths and row_penalties go with a history")
+        if history_lengths is not None:
+            keep.append(_vector(history_lengths, logits, R, "history_lengths", i32))
+            a.history_lengths = _ptr(keep[-1])
+        if row_penalties is not None:
+            rp, _ = _matrix(row_penalties, logits, 3, "row_penalties", torch.float32, rows=R)
+            keep.append(rp.contiguous())
+            a.row_penalties = _ptr(keep[-1])
+        if bias is not None:
+            m, a.ld_bias = _matrix(bias, logits, V, "bias", torch.float32, rows=R, one_row=True)
+            a.bias = _ptr(m)
+            keep.append(m)
+        if allowed is not None:
+            m, a.ld_allowed = _matrix(allowed, logits, (V + 31) // 32, "allowed", i32, rows=R,
+                                      one_row=True)
+            a.allowed = _ptr(m)
+            keep.append(m)
+        if graph is not None:
+            keep.append(_vector(states, logits, R, "states", i32))
+            a.graph, a.states = graph._h, _ptr(keep[-1])
+        if out is None:
+            out, o, ldo = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), None, V
+        else:
+            if out.shape != logits.shape:
+                raise ValueError("out must have the shape of logits")
+            o, ldo = _matrix(out, logits, V, "out")
+            if R > 0 and o.data_ptr() != out.data_ptr():
+                raise ValueError("out must have contiguous rows at one distance")
+        L = lib()
+        nbytes = L.tbs_adjust_logits_workspace(code, R, V, a.normalize)
+        ws = _workspace(nbytes, logits)
+        _check(L.tbs_adjust_logits(code, _ptr(z), ldz, R, V, ctypes.byref(a),
+                                   _ptr(out if o is None else o), ldo, _ptr(ws), nbytes,
+                                   _stream_ptr()))
+    return out
+
+
+def transducer_gradient(kind: str, blank, label, lengths, weights=None, stream=None):
+    """Log-likelihoods of ``transducer_forward`` and the gradient of
+    sum(weights * total) with respect to blank and label (tbs_transducer_gradient); weights
+    float64 [B] (None: 1 each).  Returns (total [B] float64, grad_blank [B, T, U+1],
+    grad_label [B, T, U] float32, status [B] int32); gradients are 0 outside each utterance's
+    lengths.  lengths as a device int32 tensor [B, 2] costs no host copy."""
+    import torch
+    if blank.dim() != 3 or blank.shape[2] < 1:
+        raise ValueError("blank must be [B, T, U + 1]")
+    B, T, U1 = (int(n) for n in blank.shape)
+    U, f32 = U1 - 1, torch.float32
+    if tuple(label.shape) != (B, T, U) or label.device != blank.device:
+        raise ValueError("label must be [B, T, U] beside blank [B, T, U + 1]")
+    if blank.dtype != f32 or label.dtype != f32:
+        raise ValueError("blank and label must be float32")
+    with _scope(blank, stream):
+        dev = blank.device
+        lengths = torch.as_tensor(lengths, dtype=torch.int32).reshape(B, 2).to(dev).contiguous()
+        if weights is not None:
+            weights = _vector(torch.as_tensor(weights, dtype=torch.float64, device=dev), blank, B,
+                              "weights", torch.float64)
+        blank, label = blank.contiguous(), label.contiguous()
+        total = torch.empty(B, dtype=torch.float64, device=dev)
+        status = torch.empty(B, dtype=torch.int32, device=dev)
+        grad_blank, grad_label = torch.empty_like(blank), torch.empty_like(label)
+        L = lib()
+        nbytes = L.tbs_transducer_gradient_workspace(B, T, U)
+        ws = _workspace(nbytes, blank)
+        _check(L.tbs_transducer_gradient(
+            TRANSDUCER_KINDS[kind], _ptr(blank), _ptr(label), _ptr(lengths), _ptr(weights), B, T,
+            U, _ptr(total), _ptr(grad_blank), _ptr(grad_label), _ptr(status), _ptr(ws), nbytes,
+            _stream_ptr()))
+    return total, grad_blank, grad_label, status
