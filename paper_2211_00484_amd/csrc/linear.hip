@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "types.h"
@@ -68,64 +69,79 @@ __device__ __forceinline__ float slope(float z, int act) {
   }
 }
 
-// out (and pre) of four consecutive columns n .. n+3 of row m from their sums
-template <class T>
-__device__ __forceinline__ void epilogue4(const LinearEpilogue& e, f32x4 z, int m, int n, int N) {
+// out (and pre) of E consecutive columns n .. of row m from their sums, biases and residuals
+// (FULL: all of them lie inside the row).
+template <class T, int E, bool FULL>
+__device__ __forceinline__ void finish(const LinearEpilogue& e, Vec<float, E> z, const Vec<T, E>& bias,
+                                       const Vec<T, E>& r, int m, int n, int N) {
   T* out = (T*)e.out + (size_t)m * e.ldo + n;
-  const T* res = e.res ? (const T*)e.res + (size_t)m * e.ldr + n : nullptr;
-  const T* bias = e.bias ? (const T*)e.bias + n : nullptr;
   T* pre = e.pre ? (T*)e.pre + (size_t)m * e.ldp + n : nullptr;
-  if (n + 4 <= N) {
-    f32x4 r = {0.f, 0.f, 0.f, 0.f};
-    if (res) {
-      const Vec<T, 4> t = load_vec<T, 4>(res);
+  const bool whole = FULL || n + E <= N;
+  Vec<T, E> o;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) r[v] = to_float(t.v[v]);
-    }
-    if (bias) {
-      const Vec<T, 4> t = load_vec<T, 4>(bias);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) z[v] += to_float(t.v[v]);
-    }
-    if (!e.res_after)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) z[v] += r[v];
-    Vec<T, 4> o;
-    if (pre) {
-#pragma unroll
-      for (int v = 0; v < 4; ++v) o.v[v] = from_float<T>(z[v]);
-      store_vec(pre, o);
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      float y = activate(z[v], e.act);
-      if (e.res_after) y += r[v];
-      o.v[v] = from_float<T>(y);
-    }
-    store_vec(out, o);
-  } else {
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      if (n + v >= N) break;
-      float y = z[v];
-      const float r = res ? to_float(res[v]) : 0.f;
-      if (bias) y += to_float(bias[v]);
-      if (!e.res_after) y += r;
-      if (pre) pre[v] = from_float<T>(y);
-      y = activate(y, e.act);
-      if (e.res_after) y += r;
-      out[v] = from_float<T>(y);
-    }
+  for (int v = 0; v < E; ++v) {
+    z.v[v] += to_float(bias.v[v]);
+    if (!e.res_after) z.v[v] += to_float(r.v[v]);
   }
+  auto put = [&](T* to) {
+#pragma unroll
+    for (int v = 0; v < E; ++v) o.v[v] = from_float<T>(z.v[v]);
+    if (whole) {
+      store_vec(to, o);
+    } else {
+#pragma unroll
+      for (int v = 0; v < E; ++v)
+        if (n + v < N) to[v] = o.v[v];
+    }
+  };
+  if (pre) put(pre);
+  switch (e.act) {
+    case kActRelu:
+#pragma unroll
+      for (int v = 0; v < E; ++v) z.v[v] = activate(z.v[v], kActRelu);
+      break;
+    case kActTanh:
+#pragma unroll
+      for (int v = 0; v < E; ++v) z.v[v] = activate(z.v[v], kActTanh);
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int v = 0; v < E; ++v) z.v[v] = activate(z.v[v], kActSilu);
+      break;
+    case kActGelu:
+#pragma unroll
+      for (int v = 0; v < E; ++v) z.v[v] = activate(z.v[v], kActGelu);
+      break;
+  }
+  if (e.res_after)
+#pragma unroll
+    for (int v = 0; v < E; ++v) z.v[v] += to_float(r.v[v]);
+  put(out);
+}
+// Columns n .. of a row of N (p; null: zeros, as past the row's end)
+template <class T, int E>
+__device__ __forceinline__ Vec<T, E> load_columns(const T* p, int n, int N) {
+  Vec<T, E> b = {};
+  if (!p) return b;
+  if (n + E <= N) return load_vec<T, E>(p + n);
+#pragma unroll
+  for (int v = 0; v < E; ++v)
+    if (n + v < N) b.v[v] = p[n + v];
+  return b;
+}
+template <class T, int E>
+__device__ __forceinline__ Vec<T, E> load_residual(const LinearEpilogue& e, int m, int n, int N) {
+  return load_columns<T, E>(e.res ? (const T*)e.res + (size_t)m * e.ldr : nullptr, n, N);
 }
 
 // ---------------------------------------------------------------------------
-// staging of an operand's slice: ROWS rows (m or n) x 64 bytes of k, as 16-byte chunks
+// staging of an operand's slice: ROWS rows (m or n) x 128 bytes of k, as 16-byte chunks
+// (128: a whole cache line of each row; slices of 64 bytes halve the rate of the loads)
 
 template <class T>
 constexpr int kChunkElems = 16 / (int)sizeof(T);
 template <class T>
-constexpr int kSlice = 64 / (int)sizeof(T);  // k per slice
+constexpr int kSlice = 128 / (int)sizeof(T);  // k per slice
 
 // Elements [k, k + a chunk) of a row of n, zeros past its end.  A chunk that crosses the end
 // is read from the row's last whole chunk and shifted.
@@ -149,20 +165,34 @@ __device__ __forceinline__ uint4 load_chunk_guarded(const T* row, int k, int n) 
   return v;
 }
 
-// Byte offset in an operand's stage of chunk c of tile row r (KC), or of chunk c of k row r
-// (not KC).  The chunks are permuted so that the lanes that read together meet different
-// banks: KC, 16 rows of one chunk; not KC, 16-bit, 4 k rows x 16 columns; fp32, the k rows
-// r and r + 4, r + 8, r + 12 of 16 columns.
+// Places of a slice's chunks in LDS, numbered in the order in which direct copies fill them:
+// 64 in a row by a wave, 16 bytes a lane, lanes in a row taking pieces of a cache line in a row
+// (the loads take four times as long where the lanes permute them: 148 M single accesses
+// for 134 M chunks).  So conflicts are kept off not by permuting chunks but by sharing the rows
+// out to blocks, a pad behind each:
+//  - KC: row r to block r % 8, pads of 16 bytes: 8 rows of a fragment meet 8 places;
+//  - not KC, 16-bit: k row r to block r % 4, pads of 32: a transposing read's 4 k rows x 32 bytes;
+//  - not KC, fp32: k row r to block r / 4 % 4, pads of 64: rows of two lane groups x 64 bytes.
 template <class T, bool KC, int ROWS>
-__device__ __forceinline__ int chunk_at(int r, int c) {
-  if (KC) return r * 64 + ((c ^ ((r >> 1) & 3)) * 16);
-  const int x = sizeof(T) == 2 ? (r & 3) << 1 : ((r >> 2) & 3) << 2;
-  return r * ROWS * (int)sizeof(T) + ((c ^ x) * 16);
-}
+struct Layout {
+  static constexpr int CH = kChunkElems<T>;
+  static constexpr int CPR = KC ? 8 : ROWS / CH;           // chunks per row (of k, or of m)
+  static constexpr int BLOCKS = KC ? 8 : 4, CPB = ROWS * 8 / BLOCKS;
+  static constexpr int PAD = KC ? 16 : sizeof(T) == 2 ? 32 : 64;
+  static constexpr int BLOCK = CPB * 16 + PAD, BYTES = BLOCKS * BLOCK;
+  static_assert(CPB % 64 == 0, "a wave's copy stays in a block");
+  __device__ static __forceinline__ int at(int id) { return id / CPB * BLOCK + id % CPB * 16; }
+  __device__ static __forceinline__ int row(int id) {
+    const int block = id / CPB, r = id % CPB / CPR;
+    return KC || sizeof(T) == 2 ? r * BLOCKS + block : r / 4 * 16 + block * 4 + r % 4;
+  }
+  __device__ static __forceinline__ int chunk(int id) { return id % CPR; }
+};
 
 template <class T, bool KC, int ROWS, int THREADS>
 struct Stager {
-  static constexpr int CH = kChunkElems<T>, N = ROWS * 4 / THREADS;
+  typedef Layout<T, KC, ROWS> L;
+  static constexpr int CH = kChunkElems<T>, N = ROWS * 8 / THREADS;
   uint4 r[N];
   // slice from k0 on of rows row0 .. (of `rows`), contraction length kc
   __device__ __forceinline__ void load(const T* p, long long ld, int row0, int rows, int k0, int kc) {
@@ -171,13 +201,12 @@ struct Stager {
     for (int q = 0; q < N; ++q) {
       const int id = threadIdx.x + q * THREADS;
       if (KC) {
-        const int gr = min(row0 + id / 4, rows - 1), k = k0 + id % 4 * CH;
+        const int gr = min(row0 + L::row(id), rows - 1), k = k0 + L::chunk(id) * CH;
         const T* row = p + (size_t)gr * ld;
         if (tail) r[q] = load_chunk_guarded(row, k, kc);
         else __builtin_memcpy(&r[q], row + k, 16);
       } else {
-        constexpr int CPR = ROWS / CH;
-        const int k = k0 + id / CPR, col = row0 + id % CPR * CH;
+        const int k = k0 + L::row(id), col = row0 + L::chunk(id) * CH;
         const T* row = p + (size_t)min(k, kc - 1) * ld;
         if (row0 + ROWS > rows) r[q] = load_chunk_guarded(row, col, rows);
         else __builtin_memcpy(&r[q], row + col, 16);
@@ -187,22 +216,65 @@ struct Stager {
   }
   __device__ __forceinline__ void store(char* stage) const {
 #pragma unroll
+    for (int q = 0; q < N; ++q) *reinterpret_cast<uint4*>(stage + L::at(threadIdx.x + q * THREADS)) = r[q];
+  }
+};
+
+// Copies straight into LDS: a wave's 64 chunks land in 1 KiB from `to` on, lane l's at 16 l.
+// Written as assembly (with no register to receive anything) because the compiler lets every
+// later LDS read wait for all copies of its own; the waits are in wait_copies.
+__device__ __forceinline__ void copy_chunks(unsigned to, const char* base, unsigned offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(to), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+// Waits until at most N of the wave's copies are in flight and its LDS accesses are done, then
+// for the workgroup.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+}
+
+// The same slices as Stager's by direct copies.  Chunks of rows past the operand's end are
+// those of its last row (KC) or begin in its last whole or partial chunk (not KC; what is read
+// behind a row's end is the start of the next, which exists in every slice but the last):
+// they only reach results that are not stored.
+template <class T, bool KC, int ROWS, int THREADS>
+struct Copier {
+  typedef Layout<T, KC, ROWS> L;
+  static constexpr int CH = kChunkElems<T>, N = ROWS * 8 / THREADS;
+  unsigned offset[N];
+  const char* base;
+  long long step;
+  __device__ __forceinline__ void init(const T* p, long long ld, int row0, int rows, int k0) {
+    base = (const char*)(p + (KC ? (size_t)row0 * ld + k0 : (size_t)k0 * ld + row0));
+    step = KC ? 128 : (long long)kSlice<T> * ld * (int)sizeof(T);
+#pragma unroll
     for (int q = 0; q < N; ++q) {
-      const int id = threadIdx.x + q * THREADS;
-      constexpr int CPR = KC ? 4 : ROWS / CH;
-      *reinterpret_cast<uint4*>(stage + chunk_at<T, KC, ROWS>(id / CPR, id % CPR)) = r[q];
+      const int id = threadIdx.x + q * THREADS, r = L::row(id), c = L::chunk(id);
+      if (KC) offset[q] = (unsigned)((long long)min(r, rows - 1 - row0) * ld * (int)sizeof(T)) + c * 16;
+      else offset[q] = (unsigned)((long long)r * ld * (int)sizeof(T)) + min(c, (rows - 1 - row0) / CH) * 16;
     }
+  }
+  __device__ __forceinline__ void copy(unsigned stage, int wave) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) copy_chunks(stage + L::at(q * THREADS + wave * 64), base, offset[q]);
+    base += step;
   }
 };
 
 // ---------------------------------------------------------------------------
-// fragments: lane l holds row l & 15 of a 16-row block; g = l >> 4 its share of k
+// fragments of half a slice (64 bytes of k): lane l holds row l & 15 of a 16-row block;
+// g = l >> 4 its share of k
 
 template <class T, bool KC, int ROWS>
-__device__ __forceinline__ uint4 fragment(const char* stage, int row0, int lane) {
+__device__ __forceinline__ uint4 fragment(const char* stage, int row0, int half, int lane) {
+  typedef Layout<T, KC, ROWS> L;
   const int i = lane & 15, g = lane >> 4;
   if (KC) {
-    return *reinterpret_cast<const uint4*>(stage + chunk_at<T, true, ROWS>(row0 + i, g));
+    return *reinterpret_cast<const uint4*>(stage + (i & 7) * L::BLOCK + (i >> 3) * 128 + g * 16 + row0 * 16 +
+                                           half * 64);
   } else if (sizeof(T) == 2) {
     // k rows 8 g .. 8 g + 7 of 16 columns: two transposing reads of 4 k rows each, in which
     // lane i of 16 addresses 4 columns of one k row and receives column i of the four
@@ -210,22 +282,19 @@ __device__ __forceinline__ uint4 fragment(const char* stage, int row0, int lane)
       s16x4 h[2];
       uint4 v;
     } u;
+    const char* at = stage + (i >> 2) * L::BLOCK + 2 * g * (ROWS * 2) + (i & 3) * 8 + row0 * 2 + half * 8 * (ROWS * 2);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = 8 * g + 4 * h + (i >> 2);
-      const char* at = stage + chunk_at<T, false, ROWS>(k, row0 / 8 + ((i & 3) >> 1)) + (i & 1) * 8;
-      u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-    }
+    for (int h = 0; h < 2; ++h)
+      u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + h * (ROWS * 2)));
     return u.v;
   } else {
     union {
       float f[4];
       uint4 v;
     } u;
+    const char* at = stage + g * L::BLOCK + (row0 + i) * 4 + half * 4 * (ROWS * 4);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      u.f[j] = *reinterpret_cast<const float*>(stage + chunk_at<T, false, ROWS>(4 * g + j, row0 / 4 + (i >> 2)) +
-                                               (i & 3) * 4);
+    for (int j = 0; j < 4; ++j) u.f[j] = *reinterpret_cast<const float*>(at + j * (ROWS * 4));
     return u.v;
   }
 }
@@ -258,16 +327,25 @@ __device__ __forceinline__ uint4 ones_fragment(_Float16) {
 // ---------------------------------------------------------------------------
 // the tiled product
 
+// Orders a wave's LDS accesses before and after it (the hardware runs them in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // One workgroup: a BM x BN tile of C over slices [first, last) of one of `splits` parts of k;
 // each wave WM x WN of it.  splits > 1: fp32 partial sums to part [splits][M][N] (and, rsum,
 // the sums over k of A's rows to rpart [splits][M]); else the epilogue (rsum: to rout).
-template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN>
+// DIRECT: operands whose rows are 4-byte aligned are copied straight into a ring of ST
+// slices, ST - 1 of them in flight while one is used; the last slice, where it is not whole, and
+// other operands go through registers.
+template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductArgs p) {
   constexpr int THREADS = 64 * (BM / WM) * (BN / WN);
   constexpr int MB = WM / 16, NB = WN / 16;
-  constexpr int kStage = (BM + BN) * 64;
-  __shared__ __align__(16) char lds[2 * kStage];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kA = Layout<T, AKC, BM>::BYTES, kStage = kA + Layout<T, BKC, BN>::BYTES;
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Tiles in row-major order with each XCD on a run of neighbours (workgroup i is handed to
   // XCD i mod 8), so that the tiles of one row of A meet in one L2.
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
@@ -290,68 +368,191 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const bool rsum = p.rsum && tn == 0 && wn == 0;
+  const bool rsum = !AKC && p.rsum && tn == 0 && wn == 0;
+  // The fragments of a half slice, and their products.  The second half's products are left
+  // until the first half of the next slice has been asked for, so that its LDS reads (and the
+  // wait for the workgroup before them) have products to hide behind.
+  struct Half {
+    uint4 a[MB], b[NB];
+  };
+  Half h0, h1;
+  auto read = [&](const char* cur, int h, Half& f) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) f.a[i] = fragment<T, AKC, BM>(cur, wm + 16 * i, h, lane);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) f.b[j] = fragment<T, BKC, BN>(cur + kA, wn + 16 * j, h, lane);
+  };
+  auto multiply = [&](const Half& f) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) acc[i][j] = mma(T{}, f.b[j], f.a[i], acc[i][j]);
+    if (!AKC && rsum) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) rs[i] = mma(T{}, ones_fragment(T{}), f.a[i], rs[i]);
+    }
+  };
+  constexpr bool kDeep = MB * NB <= 16;  // (larger tiles have no registers for two halves)
+  auto slice = [&](const char* cur, bool any) {
+    read(cur, 0, h0);
+    if (kDeep) {
+      if (any) multiply(h1);
+      read(cur, 1, h1);
+    } else {
+      multiply(h0);
+      read(cur, 1, h0);
+    }
+    multiply(h0);
+  };
   Stager<T, AKC, BM, THREADS> sa;
   Stager<T, BKC, BN, THREADS> sb;
-  if (first < last) {
-    sa.load(a, p.lda, m0, p.M, first * kSlice<T>, p.K);
-    sb.load(b, p.ldb, n0, p.N, first * kSlice<T>, p.K);
-    sa.store(lds);
-    sb.store(lds + BM * 64);
-  }
-  __syncthreads();
-  for (int s = first; s < last; ++s) {
-    const char* cur = lds + ((s - first) & 1) * kStage;
-    char* next = lds + (~(s - first) & 1) * kStage;
-    if (s + 1 < last) {
-      sa.load(a, p.lda, m0, p.M, (s + 1) * kSlice<T>, p.K);
-      sb.load(b, p.ldb, n0, p.N, (s + 1) * kSlice<T>, p.K);
+  auto load = [&](int s) {
+    sa.load(a, p.lda, m0, p.M, s * kSlice<T>, p.K);
+    sb.load(b, p.ldb, n0, p.N, s * kSlice<T>, p.K);
+  };
+  if (DIRECT) {
+    Copier<T, AKC, BM, THREADS> ca;
+    Copier<T, BKC, BN, THREADS> cb;
+    ca.init(a, p.lda, m0, p.M, first * kSlice<T>);
+    cb.init(b, p.ldb, n0, p.N, first * kSlice<T>);
+    constexpr int kCopies = ca.N + cb.N;
+    const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
+    // slices that copies may take: all, but for a last one that is not whole
+    const bool partial = p.K % kSlice<T> != 0 || (!AKC && p.M % kChunkElems<T> != 0) ||
+                         (!BKC && p.N % kChunkElems<T> != 0);
+    const int whole = partial ? min(last, slices - 1) : last;
+    int in = 0;  // stage that the next slice goes to
+    auto request = [&](int s) {
+      if (s < whole) {
+        ca.copy(base + in * kStage, wave);
+        cb.copy(base + in * kStage + kA, wave);
+      } else if (s < last) {
+        load(s);
+        sa.store(lds + in * kStage);
+        sb.store(lds + in * kStage + kA);
+      }
+      in = in == ST - 1 ? 0 : in + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < ST - 1; ++i) request(first + i);
+    int out = 0;
+    for (int s = first; s < last; ++s) {
+      if (s + ST - 2 < whole) wait_copies<(ST - 2) * kCopies>();
+      else wait_copies<0>();
+      request(s + ST - 1);  // (to the place of slice s - 1, which every wave has read)
+      slice(lds + out * kStage, s > first);
+      out = out == ST - 1 ? 0 : out + 1;
     }
-    uint4 fa[MB];
-#pragma unroll
-    for (int i = 0; i < MB; ++i) fa[i] = fragment<T, AKC, BM>(cur, wm + 16 * i, lane);
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const uint4 fb = fragment<T, BKC, BN>(cur + BM * 64, wn + 16 * j, lane);
-#pragma unroll
-      for (int i = 0; i < MB; ++i) acc[i][j] = mma(T{}, fb, fa[i], acc[i][j]);
-    }
-    if (rsum) {
-#pragma unroll
-      for (int i = 0; i < MB; ++i) rs[i] = mma(T{}, ones_fragment(T{}), fa[i], rs[i]);
-    }
-    if (s + 1 < last) {
-      sa.store(next);
-      sb.store(next + BM * 64);
+  } else {
+    if (first < last) {
+      load(first);
+      sa.store(lds);
+      sb.store(lds + kA);
     }
     __syncthreads();
+    for (int s = first; s < last; ++s) {
+      char* next = lds + (~(s - first) & 1) * kStage;
+      if (s + 1 < last) load(s + 1);
+      slice(lds + ((s - first) & 1) * kStage, s > first);
+      if (s + 1 < last) {
+        sa.store(next);
+        sb.store(next + kA);
+      }
+      __syncthreads();
+    }
   }
-  const int mi = lane & 15, ni = 4 * (lane >> 4);
+  if (kDeep && first < last) multiply(h1);
+  if (rsum && lane < 16) {
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int m = m0 + wm + 16 * i + mi;
-    if (m >= p.M) continue;
-    if (rsum && lane < 16) {
+    for (int i = 0; i < MB; ++i) {
+      const int m = m0 + wm + 16 * i + lane;
+      if (m >= p.M) continue;
       if (p.splits > 1) p.rpart[(size_t)split * p.M + m] = rs[i][0];
       else if (p.rout) ((T*)p.rout)[m] = from_float<T>(rs[i][0]);
     }
-    if (!p.epi.out) continue;
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int n = n0 + wn + 16 * j + ni;
-      if (n >= p.N) continue;
-      if (p.splits > 1) {
-        float* q = p.part + ((size_t)split * p.M + m) * p.N + n;
-        if (n + 4 <= p.N) {
-          __builtin_memcpy(q, &acc[i][j], 16);
-        } else {
-          for (int v = 0; n + v < p.N; ++v) q[v] = acc[i][j][v];
-        }
-      } else {
-        epilogue4<T>(p.epi, acc[i][j], m, n, p.N);
-      }
-    }
   }
+  if (!p.epi.out) return;
+  // Results leave through LDS, 16 rows of the wave's columns at a time: a lane holds 4 columns
+  // of a row, but stores (and reads the residual) in 16-byte pieces, a row's side by side.  The
+  // rows are rolled in one loop, with the registers picked by a switch: unrolled, the five
+  // activations take more code than the instruction cache holds.
+  constexpr int E = kChunkElems<T>, LPR = WN / E, RPP = 64 / LPR, RS = WN + 4;
+  __syncthreads();  // the waves have read their last slices
+  float* tile = reinterpret_cast<float*>(lds) + wave * 16 * RS;
+  const int row = lane / LPR, col = lane % LPR * E;
+  const int n = n0 + wn + col;
+  const bool parts = p.splits > 1;
+  const Vec<T, E> bias = load_columns<T, E>(parts ? nullptr : (const T*)p.epi.bias, n, p.N);
+  // Tiles that lie inside C whole take no branch per row, and those without a residual hold no
+  // loads: a wait for a load also waits for the stores before it, where a branch keeps the
+  // compiler from counting them (10.7 us for a 256 x 256 tile's results before).
+  auto leave = [&](auto full_c, auto res_c) __attribute__((always_inline)) {
+    constexpr bool FULL = decltype(full_c)::value, RES = decltype(res_c)::value;
+    constexpr int Q = 16 / RPP;
+    const T* r0 = RES ? (const T*)p.epi.res + (size_t)(m0 + wm + row) * p.epi.ldr + n : nullptr;
+    Vec<T, E> res[Q] = {};  // of the rows to come, asked for one block ahead
+    auto ask = [&](int i) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int off = 16 * min(i, MB - 1) + q * RPP, m = m0 + wm + row + off;
+        if (FULL) res[q] = load_vec<T, E>(r0 + (size_t)off * p.epi.ldr);
+        else if (m < p.M && !parts) res[q] = load_residual<T, E>(p.epi, m, n, p.N);
+      }
+    };
+    if (RES) ask(0);
+#pragma unroll 1
+    for (int i = 0; i < MB; ++i) {
+      // (each case ends in its own comment to the assembler: alike, the compiler merges the cases
+      // and makes acc an indexed array in scratch memory)
+      auto put = [&](const f32x4(&r)[NB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          *reinterpret_cast<f32x4*>(tile + (lane & 15) * RS + 16 * j + 4 * (lane >> 4)) = r[j];
+      };
+      static_assert(MB <= 8, "cases");
+      switch (i) {
+        case 0: put(acc[0]); asm volatile("; rows 0"); break;
+        case 1: put(acc[1 % MB]); asm volatile("; rows 1"); break;
+        case 2: put(acc[2 % MB]); asm volatile("; rows 2"); break;
+        case 3: put(acc[3 % MB]); asm volatile("; rows 3"); break;
+        case 4: put(acc[4 % MB]); asm volatile("; rows 4"); break;
+        case 5: put(acc[5 % MB]); asm volatile("; rows 5"); break;
+        case 6: put(acc[6 % MB]); asm volatile("; rows 6"); break;
+        default: put(acc[7 % MB]); asm volatile("; rows 7");
+      }
+      wave_sync();
+      Vec<T, E> now[Q];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) now[q] = res[q];
+      if (RES) ask(i + 1);
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int r = row + q * RPP, m = m0 + wm + 16 * i + r;
+        Vec<float, E> z;
+#pragma unroll
+        for (int v = 0; v < E; v += 4)
+          *reinterpret_cast<f32x4*>(z.v + v) = *reinterpret_cast<const f32x4*>(tile + r * RS + col + v);
+        if (!FULL && (m >= p.M || n >= p.N)) continue;
+        if ((!RES || !FULL) && parts) {
+          float* to = p.part + ((size_t)split * p.M + m) * p.N + n;
+          if (FULL || n + E <= p.N) {
+            store_vec(to, z);
+          } else {
+#pragma unroll
+            for (int v = 0; v < E; ++v)
+              if (n + v < p.N) to[v] = z.v[v];
+          }
+        } else {
+          finish<T, E, FULL>(p.epi, z, bias, now[q], m, n, p.N);
+        }
+      }
+      wave_sync();
+    }
+  };
+  const bool full = m0 + BM <= p.M && n0 + BN <= p.N;
+  if (!full) leave(std::false_type(), std::true_type());
+  else if (p.epi.res && !parts) leave(std::true_type(), std::true_type());
+  else leave(std::true_type(), std::false_type());
 }
 
 // Sum of the parts of a split product, in the parts' order, and the epilogue; the last
@@ -363,20 +564,23 @@ __global__ __launch_bounds__(256) void k_join_parts(ProductArgs p) {
   long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   if (id < total) {
     const int m = (int)(id / quads), n = (int)(id - (long long)m * quads) * 4;
-    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    Vec<float, 4> z = {};
     const float* q = p.part + (size_t)m * p.N + n;
     const size_t step = (size_t)p.M * p.N;
     if (n + 4 <= p.N) {
       for (int s = 0; s < p.splits; ++s) {
-        f32x4 t;
-        __builtin_memcpy(&t, q + s * step, 16);
-        z += t;
+        const Vec<float, 4> t = load_vec<float, 4>(q + s * step);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z.v[v] += t.v[v];
       }
     } else {
       for (int s = 0; s < p.splits; ++s)
-        for (int v = 0; n + v < p.N; ++v) z[v] += q[s * step + v];
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (n + v < p.N) z.v[v] += q[s * step + v];
     }
-    epilogue4<T>(p.epi, z, m, n, p.N);
+    finish<T, 4, false>(p.epi, z, load_columns<T, 4>((const T*)p.epi.bias, n, p.N), load_residual<T, 4>(p.epi, m, n, p.N), m,
+                 n, p.N);
     return;
   }
   id -= total;
@@ -417,20 +621,48 @@ __global__ __launch_bounds__(256) void k_act_grad(const T* __restrict__ dy, long
 
 constexpr long long kMaxTiles = 1 << 23;  // (a launch holds less than 2^32 threads)
 
-template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN>
-hipError_t launch_tile(const ProductArgs& p, hipStream_t st) {
-  const int tiles = p.tiles_m * p.tiles_n * p.splits;
-  hipLaunchKernelGGL((k_product<T, AKC, BKC, BM, BN, WM, WN>), dim3(tiles), dim3(64 * (BM / WM) * (BN / WN)), 0,
-                     st, p);
+// Whether direct copies may take an operand: rows that start on 4 bytes, offsets within a tile
+// that fit 32 bits, and, with k down its columns, rows of a chunk at least.
+template <class T>
+bool direct_ok(const void* p, long long ld, bool kc, int rows) {
+  return (uintptr_t)p % 4 == 0 && ld * (long long)sizeof(T) % 4 == 0 && ld < (1 << 20) &&
+         (kc || rows >= kChunkElems<T>);
+}
+
+template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT>
+hipError_t launch_tile_d(const ProductArgs& p, hipStream_t st) {
+  constexpr size_t lds = (DIRECT ? ST : 2) * (Layout<T, AKC, BM>::BYTES + Layout<T, BKC, BN>::BYTES);
+  if (lds > 65536) {
+    static LdsGrant grant;
+    const hipError_t e = grant((const void*)k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT>, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT>), dim3(p.tiles_m * p.tiles_n * p.splits),
+                     dim3(64 * (BM / WM) * (BN / WN)), lds, st, p);
   return hipGetLastError();
 }
 
+template <class T, bool AKC, bool BKC>
+hipError_t launch_shape(const ProductArgs& p, hipStream_t st) {
+  const bool direct = direct_ok<T>(p.a, p.lda, AKC, p.M) && direct_ok<T>(p.b, p.ldb, BKC, p.N);
+  if (p.shape == 0)
+    return direct ? launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, true>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, false>(p, st);
+  if (p.shape == 1 || sizeof(T) == 4)
+    return direct ? launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, true>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, false>(p, st);
+  if constexpr (sizeof(T) == 2)
+    return direct ? launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, true>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, false>(p, st);
+  return hipErrorInvalidValue;  // (not reached)
+}
+
 template <class T>
-hipError_t launch_product_t(ProductArgs p, bool akc, bool bkc, hipStream_t st) {
+hipError_t launch_product_t(const ProductArgs& p, bool akc, bool bkc, hipStream_t st) {
   hipError_t e;
-  if (akc && bkc) e = launch_tile<T, true, true, 64, 64, 32, 32>(p, st);
-  else if (akc) e = launch_tile<T, true, false, 64, 64, 32, 32>(p, st);
-  else e = launch_tile<T, false, false, 64, 64, 32, 32>(p, st);
+  if (akc && bkc) e = launch_shape<T, true, true>(p, st);
+  else if (akc) e = launch_shape<T, true, false>(p, st);
+  else e = launch_shape<T, false, false>(p, st);
   if (e != hipSuccess || p.splits == 1) return e;
   const long long items = (p.epi.out ? (long long)p.M * ((p.N + 3) / 4) : 0) + (p.rsum && p.rout ? p.M : 0);
   hipLaunchKernelGGL(k_join_parts<T>, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, st, p);
@@ -444,11 +676,32 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   if (p.M > kMost || p.N > kMost || p.K > kMost) return false;
   const int ks = dtype == kF32 ? kSlice<float> : kSlice<_Float16>;
   const int slices = (p.K + ks - 1) / ks;
-  p.tiles_m = (p.M + 63) / 64;
-  p.tiles_n = (p.N + 63) / 64;
-  p.splits = 1;
-  p.slices_per = std::max(slices, 1);
-  return (long long)p.tiles_m * p.tiles_n <= kMaxTiles;
+  if (((long long)p.M + 63) / 64 * (((long long)p.N + 63) / 64) > kMaxTiles) return false;
+  const int cus = device_cus() > 0 ? device_cus() : 256;
+  static const int bm[] = {64, 128, 256}, bn[] = {64, 128, 256};
+  auto tiles = [&](int s) {
+    return (long long)((p.M + bm[s] - 1) / bm[s]) * ((p.N + bn[s] - 1) / bn[s]);
+  };
+  // 256 x 256 tiles (16-bit operands) where they fill their last round of a tile per CU to three
+  // quarters: 64,000 x 512, K = 2,048 155 us against 177 by 128 x 128; 40,000 x 512, K = 500, a
+  // quarter of a second round, 46.8 against 42.9.  fp32 operands, bound by their matrix
+  // instructions, spread best in small tiles: 8,000 x 384, K = 512 31.8 us by 64 x 64, 47.2 by
+  // 128 x 128.
+  const long long rounds = (tiles(2) + cus - 1) / cus;
+  if (dtype == kF32) p.shape = tiles(1) >= 4 * cus ? 1 : 0;
+  else if (4 * tiles(2) >= 3 * rounds * cus) p.shape = 2;
+  else p.shape = tiles(1) * slices >= 8 * cus ? 1 : 0;
+  p.tiles_m = (p.M + bm[p.shape] - 1) / bm[p.shape];
+  p.tiles_n = (p.N + bn[p.shape] - 1) / bn[p.shape];
+  const long long n = tiles(p.shape);
+  long long splits = 1;
+  // Fewer tiles than CUs: k in parts of 8 slices at least, two workgroups per CU (dW of 500 x 512
+  // over 40,000 rows: 41 us in 32 parts, 66 in 8; shorter parts do not pay for the join: 512 x
+  // 512, K = 512, 15.5 us whole, 19 in 2).
+  if (n < cus) splits = std::max(1ll, std::min((2 * cus + n - 1) / n, (long long)slices / 8));
+  p.slices_per = std::max(1, (int)((slices + splits - 1) / splits));
+  p.splits = std::max(1, (slices + p.slices_per - 1) / p.slices_per);
+  return true;
 }
 
 hipError_t launch_product(const ProductArgs& p, int dtype, bool akc, bool bkc, hipStream_t st) {
