@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -216,6 +217,99 @@ __global__ __launch_bounds__(kRingThreads) void k_transducer_logs(
 }
 
 // ---------------------------------------------------------------------------
+// Gradient.  With alpha(t, u) the weight of the paths into a cell and beta(t, u) of those
+// from it to the end (as sums of products), Z the likelihood, pb = e^blank and pl = e^label,
+// d log Z / d input is the share of the paths that use the input:
+//   eq. (1)  blank(t, u): alpha(t, u) pb(t, u) beta(t+1, u) / Z (1 at the last cell),
+//            label(t, u): alpha(t, u) pl(t, u) beta(t, u+1) / Z;
+//   eq. (2)  label(t, u): alpha(t, u) pl(t, u) beta(t+1, u+1) / Z, blank as in eq. (1);
+//   eq. (3)  with g(t, u) = pb(t, u) beta(t+1, u), the weight of what follows an arrival on
+//            context u in frame t: label(t, u): alpha(t, u) pl(t, u) g(t, u+1) / Z,
+//            blank(t, u): (alpha(t, u) + pl(t, u-1) alpha(t, u-1)) g(t, u) / Z.
+// beta (and g) obey alpha's recursion with frames and labels counted from the end: with
+// j = U_b - u, step row i (see the ring) takes label row T_b - 1 - i and blank row T_b - 1 - i
+// (eq. 1, 2; for eq. (1) the cell's own, its last blank left out as a factor of all) or
+// T_b - 2 - i (eq. 3, whose last blank is a factor too).  So one kernel computes both, a
+// workgroup per utterance and direction, and a second one the shares.  A score is kept as
+// m 2^e (m a float in [0.5, 1]), so that shares lose nothing to the size of the scores.
+
+constexpr int kZeroExp = -(1 << 29);  // exponent of an unreachable cell; any below half of
+                                      // it counts as one
+constexpr float kLn2Hi = 0.69314575f, kLn2Lo = 1.42860677e-6f;  // ln 2, the first with 16 bits
+
+__device__ __forceinline__ bool reachable(int2 c) { return c.y > kZeroExp / 2; }
+__device__ __forceinline__ int2 zero_cell() { return make_int2(__float_as_int(0.5f), kZeroExp); }
+// e^v; below 2^(kZeroExp / 2) it counts as 0, above 2^(-kZeroExp / 2) as infinite
+__device__ __forceinline__ int2 log_to_cell(double v) {
+  const double t = v * 1.4426950408889634;
+  if (t <= (double)(kZeroExp / 2)) return zero_cell();
+  if (!(t < (double)(-kZeroExp / 2))) return make_int2(__float_as_int(v == v ? INFINITY : NAN), 0);
+  const double e = floor(t) + 1.0;
+  return make_int2(__float_as_int((float)exp2(t - e)), (int)e);
+}
+
+// What shares are taken of: the last cell's score z, which for eq. (1) leaves the last blank out
+// as beta does, unless the total with it is no number to divide by.
+template <int KIND>
+__device__ __forceinline__ int2 likelihood_cell(int2 z, double total) {
+  if (KIND != 0) return z;
+  const int2 all = log_to_cell(total);
+  return reachable(all) && __int_as_float(all.x) < INFINITY ? z : all;
+}
+
+// Row of blank that step row i reads, in either direction (eq. (1): for i > 0 only; eq. (3)
+// from the end: -1 for the last).
+template <int KIND, bool REV>
+__device__ __forceinline__ int blank_row(int i, int Tb) {
+  if (!REV) return KIND == 0 ? i - 1 : i;
+  return KIND == 2 ? Tb - 2 - i : Tb - 1 - i;
+}
+
+// Log-domain scores of one utterance and direction: cells [T][U + 1] of this direction,
+// state before step row i (eq. 2, 3) or of row i (eq. 1) at row i.
+template <int KIND, bool REV>
+__device__ void log_scores(const float* __restrict__ bl, const float* __restrict__ lb, int Tb, int Ub, int U,
+                           int2* __restrict__ cells, double* buf, double* __restrict__ total,
+                           int2* __restrict__ zcell) {
+  const LogAdd log_add;
+  const int tid = threadIdx.x, U1 = U + 1;
+  for (int u = tid; u <= Ub; u += kRingThreads) buf[u] = u == 0 ? 0.0 : ninf();
+  __syncthreads();
+  const int steps = Tb + (KIND == 0 ? Ub : 0);
+  for (int s = 0; s < steps; ++s) {
+    const double* prev = buf + (s & 1) * U1;
+    double* next = buf + (~s & 1) * U1;
+    for (int u = tid; u <= Ub; u += kRingThreads) {
+      const int i = KIND == 0 ? s - u : s;
+      double v = prev[u];
+      if (i >= 0 && i < Tb) {
+        if (KIND != 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
+        const int rb = blank_row<KIND, REV>(i, Tb), rl = REV ? Tb - 1 - i : i;
+        const bool use = KIND == 0 ? i > 0 : rb >= 0;
+        const double xb = use ? (double)bl[(size_t)rb * U1 + (REV ? Ub - u : u)] : 0.0;
+        double w = ninf();
+        if (u > 0) {
+          w = prev[u - 1] + (double)lb[(size_t)rl * U + (REV ? Ub - u : u - 1)];
+          if (KIND == 2) w += xb;
+        }
+        v = KIND == 0 && i == 0 ? (u == 0 ? 0.0 : ninf()) : v + xb;
+        v = log_add(v, w);
+        if (KIND == 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
+      }
+      next[u] = v;
+    }
+    __syncthreads();
+  }
+  if (!REV && tid == 0) {
+    double res = buf[(steps & 1) * U1 + Ub];
+    const int2 z = log_to_cell(res);
+    if (KIND == 0) res += (double)bl[(size_t)(Tb - 1) * U1 + Ub];
+    *zcell = likelihood_cell<KIND>(z, res);
+    *total = res;
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Linear-domain recursion.  A cell is m * 2^e with m a double in [0.5, 1) and e an int, so
 // nothing underflows (an unreachable cell has e near kZeroExp), and one cell is two
 // products, a scaled sum and a renormalisation (thirteen instructions, the scaling and
@@ -246,6 +340,7 @@ __global__ __launch_bounds__(kRingThreads) void k_transducer_logs(
 // utterance).  Sixteen waves instead of eight for batches of up to one utterance per
 // compute unit measured the same (47 us): the workers have slack.
 
+enum { kTotals, kAlpha, kCells };
 constexpr int kRingWorkers = kRingThreads - 64;
 constexpr int kRingLoads = 5;         // blank (and label) elements per worker and chunk
 // Inputs the linear domain takes: e^x is then within [2^-433, 2^73] and a term (an input
@@ -255,8 +350,6 @@ constexpr int kRingLoads = 5;         // blank (and label) elements per worker a
 // (Log-probabilities are at most 0; the room above it is for unnormalised scores.)
 constexpr float kRingMinLog = -300.f, kRingMaxLog = 50.f;
 constexpr int kMaxShift = 570;
-constexpr int kZeroExp = -(1 << 29);  // exponent of an unreachable cell; any below half of
-                                      // it counts as one
 constexpr int kRingMaxSteps = 200000; // (steps * 2 * 300 / ln 2 stays above kZeroExp / 2)
 constexpr size_t kRingLds = kMaxLds - 1024;
 
@@ -330,31 +423,37 @@ __device__ __forceinline__ double from_left(double v, double fill) {
 template <int K>
 constexpr int kRingGroup = K <= 2 ? 4 : K == 4 ? 2 : 1;
 
+// MODE: kTotals, kAlpha (alpha too), or kCells: the scores of the gradient, one workgroup per
+// utterance and direction (rev: from the end, see above), left as cells.
 // R: rows per chunk (a multiple of 2 kRingGroup<K>; R (U + 1) <= kRingLoads kRingWorkers);
 // ring: rows in LDS, a multiple of R, at least 2 R (with alpha 3 R) plus eq. (1)'s lag of
 // U / K;
 // rs: cells per ring row, at least U + 1 rounded up to K.
-template <int K, int KIND, bool ALPHA>
+template <int K, int KIND, int MODE>
 __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 : 2) void k_transducer_ring(
     const float* __restrict__ blank, const float* __restrict__ label,
     const int* __restrict__ lengths, int T, int U, double* __restrict__ total,
-    float* __restrict__ alpha, int* __restrict__ status, int R, int ring, int rs) {
+    float* __restrict__ alpha, int* __restrict__ status, int2* __restrict__ out_cells,
+    int2* __restrict__ zcell, int R, int ring, int rs) {
+  constexpr bool ALPHA = MODE == kAlpha, CELLS = MODE == kCells;
   constexpr int G = kRingGroup<K>;
   extern __shared__ __align__(16) double2 cells[];  // [ring][rs]
   __shared__ int s_bad[2];  // set in even and in odd groups of four chunks
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int b = CELLS ? blockIdx.x >> 1 : blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const bool rev = CELLS && (blockIdx.x & 1);
   int Tb, Ub;
-  if (!utterance(lengths, b, T, U, total, status, tid == 0, Tb, Ub)) return;  // uniform
+  if (!utterance(lengths, b, T, U, total, status, tid == 0 && !rev, Tb, Ub)) return;  // uniform
   const int U1 = U + 1;
   const float* bl = blank + (size_t)b * T * U1;
   const float* lb = label + (size_t)b * T * U;
+  int2* mine_cells = CELLS ? out_cells + (size_t)blockIdx.x * T * U1 : nullptr;
   constexpr int kOut = KIND == 0 ? 0 : 1;   // alpha row of step row i: i + kOut
   const int lag = KIND == 0 ? Ub / K : 0;   // rows the last lane in use is behind lane 0
   const int nchunks = (Tb + lag + R - 1) / R;
   float* al = ALPHA ? alpha + ((size_t)b * (T + 1) + kOut) * U1 : nullptr;
   const float inv_U1 = 1.f / (float)U1;
 
-  // alpha of step rows [i0, i1), left in the ring as (m, e)
+  // alpha (or the cells) of step rows [i0, i1), left in the ring as (m, e)
   auto store_rows = [&](int i0, int i1, int first, int stride) {
     i0 = max(i0, 0);
     i1 = min(i1, Tb);
@@ -365,6 +464,10 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
       if (slot >= ring) slot -= ring;
       const double2 c = cells[slot * rs + u];
       const int e = (int)(unsigned)(unsigned long long)__double_as_longlong(c.y);
+      if (CELLS) {
+        if (u <= Ub) mine_cells[(size_t)i0 * U1 + j] = make_int2(__float_as_int((float)c.x), e);
+        continue;
+      }
       al[(size_t)i0 * U1 + j] = u <= Ub && e > kZeroExp / 2 ? (float)log_cell(c.x, e) : -INFINITY;
     }
   };
@@ -406,13 +509,19 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
       const float* gb = bl + (ptrdiff_t)(i0 - 1 + kOut) * U1;
       const float* gl = lb + (ptrdiff_t)i0 * U;
       const int left = Tb - i0;
+      int bleft = left;
+      if (rev) {  // rows and cells counted from the end: element j lies j before these
+        gb = bl + (ptrdiff_t)(blank_row<KIND, true>(i0, Tb)) * U1 + Ub;
+        gl = lb + (ptrdiff_t)(Tb - 1 - i0) * U + Ub - 1;
+        if (KIND == 2) bleft = left - 1;
+      }
 #pragma unroll
       for (int q = 0; q < kRingLoads; ++q) {
         xb[q] = 0.f;
         xl[q] = 0.f;
-        if (bcell[q] >= 0 && brow[q] < left && (KIND != 0 || i0 + brow[q] > 0))
-          xb[q] = gb[w + q * kRingWorkers];
-        if (lcell[q] >= 0 && lrow[q] < left) xl[q] = gl[w + q * kRingWorkers];
+        const int j = rev ? -(w + q * kRingWorkers) : w + q * kRingWorkers;
+        if (bcell[q] >= 0 && brow[q] < bleft && (KIND != 0 || i0 + brow[q] > 0)) xb[q] = gb[j];
+        if (lcell[q] >= 0 && lrow[q] < left) xl[q] = gl[j];
       }
     };
     const ExpLogProb exp_log_prob;
@@ -452,7 +561,7 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
       if (seen(c)) end_chunk = c;  // (this chunk's work is harmless)
       if (c + 1 < nchunks) produce();
       if (c + 2 < nchunks) request((c + 2) * R);
-      if (ALPHA) store_rows((c - 1) * R - lag, c * R - lag, w, kRingWorkers);
+      if (ALPHA || CELLS) store_rows((c - 1) * R - lag, c * R - lag, w, kRingWorkers);
       if (highest > __float_as_int(kRingMaxLog) || lowest > __float_as_uint(kRingMinLog)) s_bad[c / 4 & 1] = 1;
       lds_barrier();
     }
@@ -460,7 +569,7 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
     __builtin_amdgcn_s_setprio(3);  // the other waves have slack
     const int c0 = lane * K, cells_row = (U1 + K - 1) / K * K;
     const int coff = min(c0, cells_row - K);  // lanes past the row read its last cells
-    const bool keep = ALPHA && c0 <= Ub;
+    const bool keep = (ALPHA || CELLS) && c0 <= Ub;
     double m[K];
     int e[K];
 #pragma unroll
@@ -496,6 +605,8 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
         for (int k = 0; k < K; ++k) {
           const double om = m[k];
           const int oe = e[k];
+          if (CELLS && KIND != 0 && keep)  // the state that the step starts from
+            cells[xs[g] + k] = make_double2(om, __longlong_as_double((long long)(unsigned)oe));
           const int top = max(oe, le);
           double v = scaled(KIND == 2 ? om : om * x[g][k].x, max(oe - top, -kMaxShift)) +
                      scaled(lm * x[g][k].y, max(le - top, -kMaxShift));
@@ -508,7 +619,7 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
           lm = KIND == 0 ? m[k] : om;
           le = KIND == 0 ? e[k] : oe;
         }
-        if (keep && act) {
+        if ((ALPHA || KIND == 0) && keep && act) {
 #pragma unroll
           for (int k = 0; k < K; ++k)
             cells[xs[g] + k] = make_double2(m[k], __longlong_as_double((long long)(unsigned)e[k]));
@@ -538,17 +649,27 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
         }
       double res = exp2 > kZeroExp / 2 ? __builtin_fma((double)exp2, 0.69314718055994529, log(mine)) : ninf();
       if (KIND == 0) res += (double)bl[(size_t)(Tb - 1) * U1 + Ub];
-      total[b] = res;
-      if (status) status[b] = 0;
+      if (!rev) {
+        total[b] = res;
+        if (status) status[b] = 0;
+        if (CELLS) zcell[b] = likelihood_cell<KIND>(make_int2(__float_as_int((float)mine), exp2), res);
+      }
     }
   }
   if (s_bad[0] | s_bad[1]) {  // uniform
     __syncthreads();  // the alpha rows stored so far are complete before others store theirs
+    if (CELLS) {
+      if (tid == 0 && !rev && status) status[b] = 0;
+      double* buf = reinterpret_cast<double*>(cells);
+      if (rev) log_scores<KIND, true>(bl, lb, Tb, Ub, U, mine_cells, buf, total + b, zcell + b);
+      else log_scores<KIND, false>(bl, lb, Tb, Ub, U, mine_cells, buf, total + b, zcell + b);
+      return;
+    }
     log_recursion<KIND>(blank, label, Tb, Ub, b, T, U, total, alpha, status,
                         (lds_double*)cells);
     return;
   }
-  if (ALPHA) store_rows((nchunks - 1) * R - lag, Tb, tid, kRingThreads);
+  if (ALPHA || CELLS) store_rows((nchunks - 1) * R - lag, Tb, tid, kRingThreads);
 }
 
 struct RingPlan {
@@ -587,17 +708,18 @@ RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
   return none;
 }
 
-template <int K, int KIND, bool ALPHA>
+template <int K, int KIND, int MODE>
 hipError_t launch_ring_t(const RingPlan& p, const float* blank, const float* label,
                          const int* lengths, int B, int T, int U, double* total, float* alpha,
-                         int* status, hipStream_t st) {
+                         int* status, int2* cells, int2* zcell, hipStream_t st) {
   static LdsGrant grant;
   if (p.lds > 65536) {
-    const hipError_t e = grant((const void*)k_transducer_ring<K, KIND, ALPHA>, p.lds);
+    const hipError_t e = grant((const void*)k_transducer_ring<K, KIND, MODE>, p.lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_transducer_ring<K, KIND, ALPHA>), dim3(B), dim3(kRingThreads), p.lds, st, blank,
-                     label, lengths, T, U, total, alpha, status, p.R, p.ring, p.rs);
+  hipLaunchKernelGGL((k_transducer_ring<K, KIND, MODE>), dim3(MODE == kCells ? 2 * B : B), dim3(kRingThreads),
+                     p.lds, st, blank, label, lengths, T, U, total, alpha, status, cells, zcell, p.R, p.ring,
+                     p.rs);
   return hipGetLastError();
 }
 
@@ -605,8 +727,10 @@ template <int K, int KIND>
 hipError_t launch_ring(const RingPlan& p, const float* blank, const float* label,
                        const int* lengths, int B, int T, int U, double* total, float* alpha,
                        int* status, hipStream_t st) {
-  return alpha ? launch_ring_t<K, KIND, true>(p, blank, label, lengths, B, T, U, total, alpha, status, st)
-               : launch_ring_t<K, KIND, false>(p, blank, label, lengths, B, T, U, total, alpha, status, st);
+  return alpha ? launch_ring_t<K, KIND, kAlpha>(p, blank, label, lengths, B, T, U, total, alpha, status, nullptr,
+                                                nullptr, st)
+               : launch_ring_t<K, KIND, kTotals>(p, blank, label, lengths, B, T, U, total, nullptr, status,
+                                                 nullptr, nullptr, st);
 }
 
 template <int KIND>
@@ -623,93 +747,6 @@ hipError_t launch_kind(const RingPlan& p, const float* blank, const float* label
     case 4: return launch_ring<4, KIND>(p, blank, label, lengths, B, T, U, total, alpha, status, st);
     case 8: return launch_ring<8, KIND>(p, blank, label, lengths, B, T, U, total, alpha, status, st);
     default: return launch_ring<16, KIND>(p, blank, label, lengths, B, T, U, total, alpha, status, st);
-  }
-}
-
-// ---------------------------------------------------------------------------
-// Gradient.  With alpha(t, u) the weight of the paths into a cell and beta(t, u) of those
-// from it to the end (as sums of products), Z the likelihood, pb = e^blank and pl = e^label,
-// d log Z / d input is the share of the paths that use the input:
-//   eq. (1)  blank(t, u): alpha(t, u) pb(t, u) beta(t+1, u) / Z (1 at the last cell),
-//            label(t, u): alpha(t, u) pl(t, u) beta(t, u+1) / Z;
-//   eq. (2)  label(t, u): alpha(t, u) pl(t, u) beta(t+1, u+1) / Z, blank as in eq. (1);
-//   eq. (3)  with g(t, u) = pb(t, u) beta(t+1, u), the weight of what follows an arrival on
-//            context u in frame t: label(t, u): alpha(t, u) pl(t, u) g(t, u+1) / Z,
-//            blank(t, u): (alpha(t, u) + pl(t, u-1) alpha(t, u-1)) g(t, u) / Z.
-// beta (and g) obey alpha's recursion with frames and labels counted from the end: with
-// j = U_b - u, step row i (see the ring) takes label row T_b - 1 - i and blank row T_b - 1 - i
-// (eq. 1, 2; for eq. (1) the cell's own, its last blank left out as a factor of all) or
-// T_b - 2 - i (eq. 3, whose last blank is a factor too).  So one kernel computes both, a
-// workgroup per utterance and direction, and a second one the shares.  A score is kept as
-// m 2^e (m a float in [0.5, 1]), so that shares lose nothing to the size of the scores.
-
-constexpr float kLn2Lo = 1.42860677e-6f;  // ln 2 = kLn2Hi + kLn2Lo, kLn2Hi with 16 bits
-constexpr float kLn2Hi = 0.69314575f;
-
-__device__ __forceinline__ bool reachable(int2 c) { return c.y > kZeroExp / 2; }
-__device__ __forceinline__ int2 zero_cell() { return make_int2(__float_as_int(0.5f), kZeroExp); }
-// e^v; below 2^(kZeroExp / 2) it counts as 0, above 2^(-kZeroExp / 2) as infinite
-__device__ __forceinline__ int2 log_to_cell(double v) {
-  const double t = v * 1.4426950408889634;
-  if (t <= (double)(kZeroExp / 2)) return zero_cell();
-  if (!(t < (double)(-kZeroExp / 2))) return make_int2(__float_as_int(v == v ? INFINITY : NAN), 0);
-  const double e = floor(t) + 1.0;
-  return make_int2(__float_as_int((float)exp2(t - e)), (int)e);
-}
-
-// Rows of an utterance's inputs that step row i reads, in either direction (row of blank,
-// row of label; -1: none, the input counts as probability 1 or leads nowhere).
-template <int KIND, bool REV>
-__device__ __forceinline__ int blank_row(int i, int Tb) {
-  if (!REV) return KIND == 0 ? i - 1 : i;
-  return KIND == 2 ? Tb - 2 - i : Tb - 1 - i;
-}
-
-// Log-domain scores of one utterance and direction: cells [T][U + 1] of this direction,
-// state before step row i (eq. 2, 3) or of row i (eq. 1) at row i.
-template <int KIND, bool REV>
-__device__ void log_scores(const float* __restrict__ bl, const float* __restrict__ lb, int Tb, int Ub, int U,
-                           int2* __restrict__ cells, double* buf, double* __restrict__ total,
-                           int2* __restrict__ zcell) {
-  const LogAdd log_add;
-  const int tid = threadIdx.x, U1 = U + 1;
-  for (int u = tid; u <= Ub; u += kRingThreads) buf[u] = u == 0 ? 0.0 : ninf();
-  __syncthreads();
-  const int steps = Tb + (KIND == 0 ? Ub : 0);
-  for (int s = 0; s < steps; ++s) {
-    const double* prev = buf + (s & 1) * U1;
-    double* next = buf + (~s & 1) * U1;
-    for (int u = tid; u <= Ub; u += kRingThreads) {
-      const int i = KIND == 0 ? s - u : s;
-      double v = prev[u];
-      if (i >= 0 && i < Tb) {
-        if (KIND != 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
-        const int rb = blank_row<KIND, REV>(i, Tb), rl = REV ? Tb - 1 - i : i;
-        const bool use = KIND == 0 ? i > 0 : rb >= 0;
-        const double xb = use ? (double)bl[(size_t)rb * U1 + (REV ? Ub - u : u)] : 0.0;
-        double w = ninf();
-        if (u > 0) {
-          w = prev[u - 1] + (double)lb[(size_t)rl * U + (REV ? Ub - u : u - 1)];
-          if (KIND == 2) w += xb;
-        }
-        v = KIND == 0 && i == 0 ? (u == 0 ? 0.0 : ninf()) : v + xb;
-        v = log_add(v, w);
-        if (KIND == 0) cells[(size_t)i * U1 + u] = log_to_cell(v);
-      }
-      next[u] = v;
-    }
-    __syncthreads();
-  }
-  if (!REV && tid == 0) {
-    double res = buf[(steps & 1) * U1 + Ub];
-    int2 z = log_to_cell(res);
-    if (KIND == 0) {  // the last blank is left out of z, unless it settles the matter
-      res += (double)bl[(size_t)(Tb - 1) * U1 + Ub];
-      const int2 all = log_to_cell(res);
-      if (!reachable(all) || !(__int_as_float(all.x) < INFINITY)) z = all;
-    }
-    *zcell = z;
-    *total = res;
   }
 }
 
@@ -776,33 +813,42 @@ __global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank,
     rz *= exp_parts(bl[(size_t)(Tb - 1) * U1 + Ub], k);
     ez -= k;
   }
-  for (long long at = (long long)part * kShareCells + threadIdx.x; at < n; at += 256) {
-    const int t = (int)(at / U1), u = (int)(at - (long long)t * U1);
-    float sb = 0.f, sl = 0.f;
-    if (live && t < Tb && u <= Ub) {
-      const int2 a = ca[at];
-      const int2* row = cb + (size_t)(Tb - 1 - t) * U1 + (Ub - u);  // the same frame and label
-      const bool lab = u < Ub;
-      const float xl = lab ? lb[(size_t)t * U + u] : 0.f;
-      if (KIND == 0) {
-        const bool last = t == Tb - 1;
-        if (last) sb = u == Ub ? 1.f : 0.f;
-        else sb = share(a, bl[at], row[-(ptrdiff_t)U1], rz, ez);
-      } else if (KIND == 1) {
-        sb = share(a, bl[at], row[0], rz, ez);
-      } else {
-        sb = share(a, 0.f, row[0], rz, ez);
-        if (u > 0) sb += share(ca[at - 1], lb[(size_t)t * U + u - 1], row[0], rz, ez);
+  // cells in turns of kShareCells; (t, u) of the next cell without a division
+  const int dt = 256 / U1, du = 256 - dt * U1;
+  for (long long from = (long long)part * kShareCells; from < n; from += (long long)parts * kShareCells) {
+    long long at = from + threadIdx.x;
+    int t = (int)(at / U1), u = (int)(at - (long long)t * U1);
+#pragma unroll
+    for (int q = 0; q < kShareCells / 256; ++q, at += 256, t += dt, u += du) {
+      if (u >= U1) {
+        u -= U1;
+        ++t;
       }
-      if (lab) sl = share(a, xl, row[-1], rz, ez);
-      if (bad) sb = sl = NAN;
-      sb = (float)(w * (double)sb);
-      sl = (float)(w * (double)sl);
+      if (at >= n) break;
+      float sb = 0.f, sl = 0.f;
+      if (live && t < Tb && u <= Ub) {
+        const int2 a = ca[at];
+        const int2* row = cb + (size_t)(Tb - 1 - t) * U1 + (Ub - u);  // the same frame and label
+        const bool lab = u < Ub;
+        const float xl = lab ? lb[(size_t)t * U + u] : 0.f;
+        if (KIND == 0) {
+          const bool last = t == Tb - 1;
+          if (last) sb = u == Ub ? 1.f : 0.f;
+          else sb = share(a, bl[at], row[-(ptrdiff_t)U1], rz, ez);
+        } else if (KIND == 1) {
+          sb = share(a, bl[at], row[0], rz, ez);
+        } else {
+          sb = share(a, 0.f, row[0], rz, ez);
+          if (u > 0) sb += share(ca[at - 1], lb[(size_t)t * U + u - 1], row[0], rz, ez);
+        }
+        if (lab) sl = share(a, xl, row[-1], rz, ez);
+        if (bad) sb = sl = NAN;
+        sb = (float)(w * (double)sb);
+        sl = (float)(w * (double)sl);
+      }
+      gb[at] = sb;
+      if (u < U) gl[(size_t)t * U + u] = sl;
     }
-    gb[at] = sb;
-    if (u < U) gl[(size_t)t * U + u] = sl;
-    if (((at + 256) & ~(long long)(kShareCells - 1)) != (at & ~(long long)(kShareCells - 1)))
-      at += (long long)(parts - 1) * kShareCells;
   }
 }
 
@@ -810,9 +856,24 @@ template <int KIND>
 hipError_t launch_gradient(const float* blank, const float* label, const int* lengths, const double* weights, int B,
                            int T, int U, double* total, float* grad_blank, float* grad_label, int* status,
                            int2* cells, int2* zcell, hipStream_t st) {
-  hipLaunchKernelGGL(k_scores_logs<KIND>, dim3(2 * B), dim3(kRingThreads), 0, st, blank, label, lengths, T, U,
-                     total, status, cells, zcell);
-  hipError_t e = hipGetLastError();
+  const RingPlan p = plan_ring(KIND, 2 * B, T, U, true, device_cus());
+  auto ring = [&](auto k) {
+    return launch_ring_t<decltype(k)::value, KIND, kCells>(p, blank, label, lengths, B, T, U, total, nullptr, status,
+                                                           cells, zcell, st);
+  };
+  hipError_t e = hipSuccess;
+  switch (p.K) {
+    case 0:
+      hipLaunchKernelGGL(k_scores_logs<KIND>, dim3(2 * B), dim3(kRingThreads), 0, st, blank, label, lengths, T, U,
+                         total, status, cells, zcell);
+      e = hipGetLastError();
+      break;
+    case 1: e = ring(std::integral_constant<int, 1>()); break;
+    case 2: e = ring(std::integral_constant<int, 2>()); break;
+    case 4: e = ring(std::integral_constant<int, 4>()); break;
+    case 8: e = ring(std::integral_constant<int, 8>()); break;
+    default: e = ring(std::integral_constant<int, 16>());
+  }
   if (e != hipSuccess) return e;
   const long long n = (long long)T * (U + 1);
   const long long want = (n + kShareCells - 1) / kShareCells, most = std::max(1, (1 << 22) / B);
