@@ -555,6 +555,65 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
   else leave(std::true_type(), std::false_type());
 }
 
+// Few rows (M <= 32: a decoder's step, a short chunk), both operands with k along their rows: a
+// workgroup per 16 columns, its four waves taking turns at the 64-byte pieces of k, straight from
+// memory to fragments with four pieces of each row in flight; their sums meet in LDS.  Bound by
+// the latency of a launch and of two or three memory round trips.
+template <class T, int MB>
+__global__ __launch_bounds__(256) void k_product_rows(ProductArgs p) {
+  constexpr int CH = kChunkElems<T>, STEP = 4 * CH, AHEAD = 4;
+  __shared__ f32x4 sums[4][MB][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const T* b = (const T*)p.b + (size_t)min(n0 + i, p.N - 1) * p.ldb;
+  const T* a[MB];
+  f32x4 acc[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    a[m] = (const T*)p.a + (size_t)min(16 * m + i, p.M - 1) * p.lda;
+    acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int whole = p.K / STEP;  // pieces without an end of a row in them
+  for (int s = wave; s < whole; s += 4 * AHEAD) {
+    uint4 fb[AHEAD], fa[AHEAD][MB];
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) {
+      const int k = min(s + 4 * t, whole - 1) * STEP + g * CH;  // (a piece too many is dropped below)
+      __builtin_memcpy(&fb[t], b + k, 16);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) __builtin_memcpy(&fa[t][m], a[m] + k, 16);
+    }
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t)
+      if (s + 4 * t < whole)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) acc[m] = mma(T{}, fb[t], fa[t][m], acc[m]);
+  }
+  if (whole * STEP < p.K && wave == whole % 4) {
+    const int k = whole * STEP + g * CH;
+    const uint4 fb = load_chunk_guarded(b, k, p.K);
+#pragma unroll
+    for (int m = 0; m < MB; ++m) acc[m] = mma(T{}, fb, load_chunk_guarded(a[m], k, p.K), acc[m]);
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) sums[wave][m][lane] = acc[m];
+  __syncthreads();
+  const int n = n0 + 4 * g;
+  if (n >= p.N) return;
+  const Vec<T, 4> bias = load_columns<T, 4>((const T*)p.epi.bias, n, p.N);
+  if (const int m = wave; m < MB) {
+    const int r = 16 * m + i;
+    if (r >= p.M) return;
+    Vec<float, 4> z;
+    f32x4 t = sums[0][m][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) t += sums[w][m][lane];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) z.v[v] = t[v];
+    finish<T, 4, false>(p.epi, z, bias, load_residual<T, 4>(p.epi, r, n, p.N), r, n, p.N);
+  }
+}
+
 // Sum of the parts of a split product, in the parts' order, and the epilogue; the last
 // workgroups sum the rows' sums.
 template <class T>
@@ -657,8 +716,19 @@ hipError_t launch_shape(const ProductArgs& p, hipStream_t st) {
   return hipErrorInvalidValue;  // (not reached)
 }
 
+constexpr int kRowsShape = 3;
+
+template <class T>
+hipError_t launch_rows(const ProductArgs& p, hipStream_t st) {
+  const dim3 grid(p.tiles_n), block(256);
+  if (p.M <= 16) hipLaunchKernelGGL((k_product_rows<T, 1>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((k_product_rows<T, 2>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t launch_product_t(const ProductArgs& p, bool akc, bool bkc, hipStream_t st) {
+  if (p.shape == kRowsShape) return launch_rows<T>(p, st);
   hipError_t e;
   if (akc && bkc) e = launch_shape<T, true, true>(p, st);
   else if (akc) e = launch_shape<T, true, false>(p, st);
@@ -678,6 +748,15 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   const int slices = (p.K + ks - 1) / ks;
   if (((long long)p.M + 63) / 64 * (((long long)p.N + 63) / 64) > kMaxTiles) return false;
   const int cus = device_cus() > 0 ? device_cus() : 256;
+  p.splits = 1;
+  // (64 rows, K = 2,048: 12.2 us by rows, 7.7 by tiles in parts; 16 rows, K = 512, N = 5,000 4.0)
+  if (akc && bkc && (p.M <= 16 || (p.M <= 32 && p.K <= 1024))) {
+    p.shape = kRowsShape;
+    p.tiles_m = 1;
+    p.tiles_n = (p.N + 15) / 16;
+    p.slices_per = std::max(slices, 1);
+    return true;
+  }
   static const int bm[] = {64, 128, 256}, bn[] = {64, 128, 256};
   auto tiles = [&](int s) {
     return (long long)((p.M + bm[s] - 1) / bm[s]) * ((p.N + bn[s] - 1) / bn[s]);

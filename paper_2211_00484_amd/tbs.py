@@ -642,10 +642,12 @@ def transducer_forward(kind: str, blank, label, lengths, want_alpha: bool = Fals
     return total, alpha, status
 
 
-# Element types by the names torch gives them.
-_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_DTYPES = {}  # tbs_dtype of torch's dtypes (filled once torch is there)
 ACTIVATIONS = {"none": 0, "relu": 1, "tanh": 2, "silu": 3, "gelu": 4}
 _I32_MAX = 2 ** 31 - 1
+
+
+_HERE_SCOPE = contextlib.nullcontext()
 
 
 def _scope(t, stream):
@@ -659,13 +661,16 @@ def _scope(t, stream):
         if stream.device != t.device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
         return torch.cuda.stream(stream)
-    if t.device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
+    if t.get_device() == torch.cuda.current_device():
+        return _HERE_SCOPE
     return torch.cuda.device(t.device)
 
 
 def _dtype_code(t) -> int:
-    code = _DTYPES.get(str(t.dtype))
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"unsupported dtype {t.dtype}: float32, bfloat16 or float16")
     return code
@@ -675,13 +680,17 @@ def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False)
     """(2-D tensor, row length) of ``t`` [..., cols]: a view where its rows are contiguous
     and no closer than their width, else a copy.  With one_row, a [cols] or [1, cols] tensor
     stands for all rows (row length 0)."""
-    if t.device != like.device:
+    dtype = dtype or like.dtype
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if t.dtype != (dtype or like.dtype):
-        raise ValueError(f"{name} must be {dtype or like.dtype}, not {t.dtype}")
-    if t.dim() == 0 or t.shape[-1] != cols:
-        raise ValueError(f"{name} must have {cols} columns, not shape {tuple(t.shape)}")
-    m = t if t.dim() == 2 else t.reshape(-1, cols)
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    shape = t.shape
+    if len(shape) == 0 or shape[-1] != cols:
+        raise ValueError(f"{name} must have {cols} columns, not shape {tuple(shape)}")
+    if len(shape) == 2 and shape[0] == rows and t.is_contiguous():
+        return t, cols
+    m = t if len(shape) == 2 else t.reshape(-1, cols)
     n = m.shape[0]
     if rows is not None and n != rows and not (one_row and n == 1):
         raise ValueError(f"{name} must have {rows} rows, not {n}")
@@ -695,14 +704,23 @@ def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False)
 
 
 def _vector(t, like, n: int, name: str, dtype=None):
-    if t.device != like.device or t.dtype != (dtype or like.dtype) or tuple(t.shape) != (n,):
-        raise ValueError(f"{name} must be {dtype or like.dtype} [{n}] on {like.device}, not "
-                         f"{t.dtype} {list(t.shape)} on {t.device}")
+    dtype = dtype or like.dtype
+    if t.get_device() != like.get_device() or t.dtype is not dtype or tuple(t.shape) != (n,):
+        raise ValueError(f"{name} must be {dtype} [{n}] on {like.device}, not {t.dtype} "
+                         f"{list(t.shape)} on {t.device}")
     return t.contiguous()
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _stream_of(t, stream):
+    """The hipStream_t inside _scope(t, stream)."""
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _workspace(nbytes: int, like):
@@ -743,7 +761,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none",
         ws = _workspace(nbytes, x)
         _check(L.tbs_linear(code, _ptr(x2), ldx, _ptr(w2), ldw, _ptr(b), _ptr(r), ldr,
                             int(residual_after), act, M, N, K, _ptr(out), N, _ptr(pre), N,
-                            _ptr(ws), nbytes, _stream_ptr()))
+                            _ptr(ws), nbytes, _stream_of(x, stream)))
     return (out, pre) if want_pre else out
 
 
@@ -788,7 +806,8 @@ def linear_backward(grad_out, x, weight, pre=None, activation: str = "none",
         ws = _workspace(nbytes, grad_out)
         _check(L.tbs_linear_backward(code, _ptr(g), ldg, _ptr(x2), ldx, _ptr(w2), ldw, _ptr(p),
                                      ldp, act, M, N, K, _ptr(dx), K, _ptr(dw), K, _ptr(db),
-                                     _ptr(dz), N, _ptr(ws), nbytes, _stream_ptr()))
+                                     _ptr(dz), N, _ptr(ws), nbytes,
+                                     _stream_of(grad_out, stream)))
     return LinearGrads(x=dx, weight=dw, bias=db,
                        pre=(dz if act else grad_out) if want_pre else None)
 
@@ -858,7 +877,7 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
         ws = _workspace(nbytes, logits)
         _check(L.tbs_adjust_logits(code, _ptr(z), ldz, R, V, ctypes.byref(a),
                                    _ptr(out if o is None else o), ldo, _ptr(ws), nbytes,
-                                   _stream_ptr()))
+                                   _stream_of(logits, stream)))
     return out
 
 
@@ -893,5 +912,5 @@ def transducer_gradient(kind: str, blank, label, lengths, weights=None, stream=N
         _check(L.tbs_transducer_gradient(
             TRANSDUCER_KINDS[kind], _ptr(blank), _ptr(label), _ptr(lengths), _ptr(weights), B, T,
             U, _ptr(total), _ptr(grad_blank), _ptr(grad_label), _ptr(status), _ptr(ws), nbytes,
-            _stream_ptr()))
+            _stream_of(blank, stream)))
     return total, grad_blank, grad_label, status
