@@ -1958,7 +1958,7 @@ void place_parts(ProductArgs& p, void* at) {
 
 size_t tbs_transducer_gradient_workspace(int32_t B, int32_t T, int32_t U) {
   if (B < 1 || T < 1 || U < 0) return 0;
-  return (transducer_cells(B, T, U) + B) * sizeof(int2);
+  return (transducer_cells(B, T, U) + transducer_zcells(B)) * sizeof(int2) + transducer_probs(B, T, U);
 }
 
 tbs_status tbs_transducer_gradient(int32_t kind, const float* blank, const float* label,

@@ -341,8 +341,16 @@ hipError_t launch_transducer_forward(int kind, const float* blank, const float* 
                                      float* alpha, int* status, hipStream_t st);
 
 // Gradient of the transducer losses with respect to the inputs: weights[b] d total[b].
-// cells: workspace of transducer_cells(B, T, U) entries; zcell: [B].
+// cells: workspace of transducer_cells(B, T, U) entries; zcell: [transducer_zcells(B)], with
+// transducer_probs bytes behind it.
 inline size_t transducer_cells(int B, int T, int U) { return (size_t)2 * B * T * (U + 1); }
+inline size_t transducer_zcells(int B) { return (size_t)(B + 1) / 2 * 2; }
+// exponentials of the inputs and flags of each utterance's parts, for batches that may run with
+// several chain waves (a workgroup per utterance and direction on at most 256 CUs)
+constexpr int kTransducerProbParts = 128;
+inline size_t transducer_probs(int B, int T, int U) {
+  return B <= 128 ? (size_t)B * T * (2 * (size_t)U + 1) * sizeof(double) + (size_t)B * kTransducerProbParts * sizeof(int) : 0;
+}
 hipError_t launch_transducer_gradient(int kind, const float* blank, const float* label, const int* lengths,
                                       const double* weights, int B, int T, int U, double* total,
                                       float* grad_blank, float* grad_label, int* status, int2* cells,

@@ -627,10 +627,15 @@ __global__ __launch_bounds__(256) void k_join_parts(ProductArgs p) {
     const float* q = p.part + (size_t)m * p.N + n;
     const size_t step = (size_t)p.M * p.N;
     if (n + 4 <= p.N) {
-      for (int s = 0; s < p.splits; ++s) {
-        const Vec<float, 4> t = load_vec<float, 4>(q + s * step);
+      for (int s = 0; s < p.splits; s += 8) {  // (eight parts in flight)
+        Vec<float, 4> t[8];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) z.v[v] += t.v[v];
+        for (int i = 0; i < 8; ++i) t[i] = load_vec<float, 4>(q + min(s + i, p.splits - 1) * step);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (s + i < p.splits)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) z.v[v] += t[i].v[v];
       }
     } else {
       for (int s = 0; s < p.splits; ++s)

@@ -273,13 +273,13 @@ __device__ void log_scores(const float* __restrict__ bl, const float* __restrict
                            int2* __restrict__ zcell) {
   const LogAdd log_add;
   const int tid = threadIdx.x, U1 = U + 1;
-  for (int u = tid; u <= Ub; u += kRingThreads) buf[u] = u == 0 ? 0.0 : ninf();
+  for (int u = tid; u <= Ub; u += (int)blockDim.x) buf[u] = u == 0 ? 0.0 : ninf();
   __syncthreads();
   const int steps = Tb + (KIND == 0 ? Ub : 0);
   for (int s = 0; s < steps; ++s) {
     const double* prev = buf + (s & 1) * U1;
     double* next = buf + (~s & 1) * U1;
-    for (int u = tid; u <= Ub; u += kRingThreads) {
+    for (int u = tid; u <= Ub; u += (int)blockDim.x) {
       const int i = KIND == 0 ? s - u : s;
       double v = prev[u];
       if (i >= 0 && i < Tb) {
@@ -423,20 +423,56 @@ __device__ __forceinline__ double from_left(double v, double fill) {
 template <int K>
 constexpr int kRingGroup = K <= 2 ? 4 : K == 4 ? 2 : 1;
 
+// NW > 1 (cells of eq. (2), (3); few utterances, whose time is the chain's): NW chain waves side
+// by side, wave v with cells 64 K v .. and a chunk behind wave v - 1, whose states before each
+// step lie in the ring by then: fewer cells per lane, a shorter step (T = 1,000, U = 150, B = 1:
+// one wave of 4 cells a lane 291 us, three of one cell 147; B = 32, T = 250, U = 80: 44, 29).
 // MODE: kTotals, kAlpha (alpha too), or kCells: the scores of the gradient, one workgroup per
 // utterance and direction (rev: from the end, see above), left as cells.
 // R: rows per chunk (a multiple of 2 kRingGroup<K>; R (U + 1) <= kRingLoads kRingWorkers);
 // ring: rows in LDS, a multiple of R, at least 2 R (with alpha 3 R) plus eq. (1)'s lag of
 // U / K;
 // rs: cells per ring row, at least U + 1 rounded up to K.
-template <int K, int KIND, int MODE>
-__global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 : 2) void k_transducer_ring(
+// e^x of every input (T (2 U + 1) per utterance, blank then label) for the ring with several chain
+// waves, whose time on one CU would be its workers' exponentials: T = 1,000, U = 150, B = 1 216 us
+// with them. flags: per part of an utterance, whether an input is none that the ring takes.
+constexpr int kProbParts = kTransducerProbParts;
+constexpr bool ring_takes_probs(int K, int NW) { return NW > 2 || (NW == 2 && K > 1); }
+__global__ __launch_bounds__(256) void k_probs(const float* __restrict__ blank, const float* __restrict__ label,
+                                               const int* __restrict__ lengths, int B, int T, int U,
+                                               double* __restrict__ probs) {
+  __shared__ int s_flag;
+  const int b = blockIdx.x / kProbParts, part = blockIdx.x % kProbParts, U1 = U + 1;
+  int* flags = reinterpret_cast<int*>(probs + (size_t)B * T * (U1 + U));
+  const int Tb = min(lengths[2 * b], T), Ub = min(lengths[2 * b + 1], U);
+  const ExpLogProb exp_log_prob;
+  if (threadIdx.x == 0) s_flag = 0;
+  __syncthreads();
+  bool bad = false;
+  auto rows = [&](const float* in, double* out, int width, int used) {
+    for (int t = part; t < Tb; t += kProbParts)
+      for (int u = threadIdx.x; u < used; u += 256) {
+        const float x = in[(size_t)t * width + u];
+        bad |= !(x >= kRingMinLog && x <= kRingMaxLog);
+        out[(size_t)t * width + u] = exp_log_prob(x);
+      }
+  };
+  rows(blank + (size_t)b * T * U1, probs + (size_t)b * T * U1, U1, Ub + 1);
+  rows(label + (size_t)b * T * U, probs + (size_t)B * T * U1 + (size_t)b * T * U, U, Ub);
+  if (bad) s_flag = 1;
+  __syncthreads();
+  if (threadIdx.x == 0) flags[blockIdx.x] = s_flag;
+}
+
+template <int K, int KIND, int MODE, int NW>
+__global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND == 0)) ? 2 : 4) void k_transducer_ring(
     const float* __restrict__ blank, const float* __restrict__ label,
     const int* __restrict__ lengths, int T, int U, double* __restrict__ total,
     float* __restrict__ alpha, int* __restrict__ status, int2* __restrict__ out_cells,
-    int2* __restrict__ zcell, int R, int ring, int rs) {
+    int2* __restrict__ zcell, const double* __restrict__ probs, int R, int ring, int rs) {
   constexpr bool ALPHA = MODE == kAlpha, CELLS = MODE == kCells;
   constexpr int G = kRingGroup<K>;
+  constexpr int W = kRingThreads - 64 * NW;  // workers
   extern __shared__ __align__(16) double2 cells[];  // [ring][rs]
   __shared__ int s_bad[2];  // set in even and in odd groups of four chunks
   const int b = CELLS ? blockIdx.x >> 1 : blockIdx.x, tid = threadIdx.x, lane = tid & 63;
@@ -472,17 +508,35 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
     }
   };
 
-  if (tid < 2) s_bad[tid] = 0;
+  constexpr bool PROBS = ring_takes_probs(K, NW);
+  const double* pbl = PROBS ? probs + (size_t)b * T * U1 : nullptr;
+  const double* plb = PROBS ? probs + (size_t)gridDim.x / 2 * T * U1 + (size_t)b * T * U : nullptr;
+  if (PROBS) {
+    const int* bad = reinterpret_cast<const int*>(probs + (size_t)gridDim.x / 2 * T * (U1 + U)) + b * kProbParts;
+    if (tid < 2) s_bad[tid] = 0;
+    __syncthreads();
+    if (tid < kProbParts && bad[tid]) s_bad[0] = 1;
+    __syncthreads();
+    if (s_bad[0]) {  // uniform
+      if (tid == 0 && !rev && status) status[b] = 0;
+      double* buf = reinterpret_cast<double*>(cells);
+      if (rev) log_scores<KIND, true>(bl, lb, Tb, Ub, U, mine_cells, buf, total + b, zcell + b);
+      else log_scores<KIND, false>(bl, lb, Tb, Ub, U, mine_cells, buf, total + b, zcell + b);
+      return;
+    }
+  } else if (tid < 2) {
+    s_bad[tid] = 0;
+  }
   // An input the linear domain does not take ends both loops within the next group of chunks:
   // while a group reads the flag of the one before, only its own can be set, so all waves
   // see the same.  (Not for eq. (1): the check alone costs its loop 3%, and its fallback is
   // shorter than what it replaces by more than the ring's pass.)
-  int end_chunk = nchunks;
+  int end_chunk = nchunks + NW - 1;
   auto seen = [&](int c) {
     return KIND != 0 && c > 0 && c % 4 == 0 && __builtin_amdgcn_readfirstlane(s_bad[~(c / 4) & 1]) != 0;
   };
-  if (tid >= 64) {
-    // Worker w handles elements j = w, w + kRingWorkers, ... of a chunk's R x U1 blank and
+  if (tid >= 64 * NW) {
+    // Worker w handles elements j = w, w + W, ... of a chunk's R x U1 blank and
     // R x U label values.  A chunk's rows are consecutive in memory and (ring being a
     // multiple of R) in the ring, so element q keeps its offset within the chunk: its
     // index in memory, its cell in the ring and its row never change.
@@ -491,13 +545,20 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
     // that is unreachable (label into cell 0, blank into row 0 of eq. 1), which keeps
     // every term a positive normal number.  The exception is eq. (1)'s first cell, whose
     // blank from a virtual row above it does have probability 1.
-    const int w = tid - 64;
-    int bcell[kRingLoads], lcell[kRingLoads];  // ring cell of element q within the chunk
-    int brow[kRingLoads], lrow[kRingLoads];    // its row (past every Tb: never read)
-    float xb[kRingLoads], xl[kRingLoads];
+    const int w = tid - 64 * NW;
+    // Inputs are asked for D chunks ahead of the one they are turned into: one where a chunk
+    // takes the chain longer than a memory round trip, more for the short chunks of several
+    // waves, with loads that no branch surrounds (the waits then count the ones in flight) and
+    // the exponentials taken beforehand (k_probs).
+    constexpr int L = kRingLoads, D = NW == 1 ? 1 : 2;
+    typedef std::conditional_t<PROBS, double, float> In;
+    int bcell[L], lcell[L];  // ring cell of element q within the chunk
+    int brow[L], lrow[L];    // its row (past every Tb: never read)
+    In xb[D][L], xl[D][L];
+    unsigned read[D];        // (D > 1) bits 2 q, 2 q + 1: blank, label q is an input
 #pragma unroll
-    for (int q = 0; q < kRingLoads; ++q) {
-      const int j = w + q * kRingWorkers;
+    for (int q = 0; q < L; ++q) {
+      const int j = w + q * W;
       const int rb = j / U1, ub = j - rb * U1;
       const int rl = U > 0 ? j / U : R, ul = j - rl * U + 1;  // the label leads to cell ul
       bcell[q] = rb < R ? rb * rs + ub : -1;
@@ -505,23 +566,42 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
       brow[q] = ub <= Ub ? rb : kRingMaxSteps;
       lrow[q] = ul <= Ub ? rl : kRingMaxSteps;
     }
-    auto request = [&](int i0) {
-      const float* gb = bl + (ptrdiff_t)(i0 - 1 + kOut) * U1;
-      const float* gl = lb + (ptrdiff_t)i0 * U;
+    auto request = [&](auto set, int i0) {
+      constexpr int d = decltype(set)::value;
+      if (D > 1) read[d] = 0;
+      const In *gb, *gl, *any;
+      if constexpr (!PROBS) {
+        gb = any = bl;
+        gl = lb;
+      } else {
+        gb = any = pbl;
+        gl = plb;
+      }
       const int left = Tb - i0;
       int bleft = left;
       if (rev) {  // rows and cells counted from the end: element j lies j before these
-        gb = bl + (ptrdiff_t)(blank_row<KIND, true>(i0, Tb)) * U1 + Ub;
-        gl = lb + (ptrdiff_t)(Tb - 1 - i0) * U + Ub - 1;
+        gb += (ptrdiff_t)(blank_row<KIND, true>(i0, Tb)) * U1 + Ub;
+        gl += (ptrdiff_t)(Tb - 1 - i0) * U + Ub - 1;
         if (KIND == 2) bleft = left - 1;
+      } else {
+        gb += (ptrdiff_t)(i0 - 1 + kOut) * U1;
+        gl += (ptrdiff_t)i0 * U;
       }
 #pragma unroll
-      for (int q = 0; q < kRingLoads; ++q) {
-        xb[q] = 0.f;
-        xl[q] = 0.f;
-        const int j = rev ? -(w + q * kRingWorkers) : w + q * kRingWorkers;
-        if (bcell[q] >= 0 && brow[q] < bleft && (KIND != 0 || i0 + brow[q] > 0)) xb[q] = gb[j];
-        if (lcell[q] >= 0 && lrow[q] < left) xl[q] = gl[j];
+      for (int q = 0; q < L; ++q) {
+        const int j = rev ? -(w + q * W) : w + q * W;
+        const bool rb = bcell[q] >= 0 && brow[q] < bleft && (KIND != 0 || i0 + brow[q] > 0);
+        const bool rl = lcell[q] >= 0 && lrow[q] < left;
+        if (D > 1) {
+          xb[d][q] = *(rb ? gb + j : any);
+          xl[d][q] = *(rl ? gl + j : any);
+          read[d] |= (rb ? 1u : 0u) << (2 * q) | (rl ? 2u : 0u) << (2 * q);
+        } else {
+          xb[d][q] = 0.f;
+          xl[d][q] = 0.f;
+          if (rb) xb[d][q] = gb[j];
+          if (rl) xl[d][q] = gl[j];
+        }
       }
     };
     const ExpLogProb exp_log_prob;
@@ -534,40 +614,85 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
       lowest = max(lowest, __float_as_uint(x));
     };
     int c0 = 0;          // ring cell of the next chunk's first row
-    auto produce = [&]() {
+    auto produce = [&](auto set) {
+      constexpr int d = decltype(set)::value;
 #pragma unroll
-      for (int q = 0; q < kRingLoads; ++q) {
-        if (bcell[q] >= 0) {
-          note(xb[q]);
-          reinterpret_cast<double*>(cells + c0 + bcell[q])[0] = exp_log_prob(xb[q]);
-        }
-        if (lcell[q] >= 0) {
-          note(xl[q]);
-          reinterpret_cast<double*>(cells + c0 + lcell[q])[1] = exp_log_prob(xl[q]);
+      for (int q = 0; q < L; ++q) {
+        if constexpr (!PROBS) {
+          const float vb = D == 1 || (read[d] >> (2 * q) & 1) ? xb[d][q] : 0.f;
+          const float vl = D == 1 || (read[d] >> (2 * q) & 2) ? xl[d][q] : 0.f;
+          if (bcell[q] >= 0) {
+            note(vb);
+            reinterpret_cast<double*>(cells + c0 + bcell[q])[0] = exp_log_prob(vb);
+          }
+          if (lcell[q] >= 0) {
+            note(vl);
+            reinterpret_cast<double*>(cells + c0 + lcell[q])[1] = exp_log_prob(vl);
+          }
+        } else {
+          if (bcell[q] >= 0)
+            reinterpret_cast<double*>(cells + c0 + bcell[q])[0] = read[d] >> (2 * q) & 1 ? xb[d][q] : 1.0;
+          if (lcell[q] >= 0)
+            reinterpret_cast<double*>(cells + c0 + lcell[q])[1] = read[d] >> (2 * q) & 2 ? xl[d][q] : 1.0;
         }
       }
-      for (int r = w; r < R; r += kRingWorkers)  // no label leads to cell 0
+      for (int r = w; r < R; r += W)  // no label leads to cell 0
         reinterpret_cast<double*>(cells + c0 + r * rs)[1] = 1.0;
       c0 += R * rs;
       if (c0 == ring * rs) c0 = 0;
     };
-    request(0);
+    std::integral_constant<int, 0> set0;
+    request(set0, 0);
     if (ALPHA && KIND != 0)  // alpha row 0
-      for (int u = w; u < U1; u += kRingWorkers) (al - U1)[u] = u == 0 ? 0.f : -INFINITY;
-    produce();
-    request(R);
-    lds_barrier();
-    for (int c = 0; c < end_chunk; ++c) {
+      for (int u = w; u < U1; u += W) (al - U1)[u] = u == 0 ? 0.f : -INFINITY;
+    produce(set0);
+    // chunk c + 1 lies in set c % D when iteration c begins
+    auto ahead = [&](auto set, int c) {
+      if (D == 1 || c < nchunks) request(set, c * R);
+    };
+    int s0 = 0;  // ring cell of the next chunk to store
+    auto store_chunk = [&](int c) {  // (as store_rows, by the elements' places)
+      if (c < 0) return;
+      int2* to = mine_cells + (size_t)c * R * U1;
+      const int left = Tb - c * R;
+#pragma unroll
+      for (int q = 0; q < L; ++q)
+        if (bcell[q] >= 0 && brow[q] < left) {
+          const double2 x = cells[s0 + bcell[q]];
+          to[w + q * W] = make_int2(__float_as_int((float)x.x),
+                                    (int)(unsigned)(unsigned long long)__double_as_longlong(x.y));
+        }
+      s0 += R * rs;
+      if (s0 == ring * rs) s0 = 0;
+    };
+    auto turn = [&](auto set, int c) {
       if (seen(c)) end_chunk = c;  // (this chunk's work is harmless)
-      if (c + 1 < nchunks) produce();
-      if (c + 2 < nchunks) request((c + 2) * R);
-      if (ALPHA || CELLS) store_rows((c - 1) * R - lag, c * R - lag, w, kRingWorkers);
+      if (c + 1 < nchunks) produce(set);
+      if (c + 1 + D < nchunks) request(set, (c + 1 + D) * R);
+      if constexpr (NW > 1) store_chunk(c - NW);
+      else if (ALPHA || CELLS) store_rows((c - 1) * R - lag, c * R - lag, w, W);
       if (highest > __float_as_int(kRingMaxLog) || lowest > __float_as_uint(kRingMinLog)) s_bad[c / 4 & 1] = 1;
       lds_barrier();
+    };
+    ahead(set0, 1);
+    if constexpr (D > 1) {
+      std::integral_constant<int, 1> set1;
+      ahead(set1, 2);
+      lds_barrier();
+      for (int c = 0; c < end_chunk;) {
+        turn(set0, c);
+        if (++c >= end_chunk) break;
+        turn(set1, c);
+        ++c;
+      }
+    } else {
+      lds_barrier();
+      for (int c = 0; c < end_chunk; ++c) turn(set0, c);
     }
   } else {
     __builtin_amdgcn_s_setprio(3);  // the other waves have slack
-    const int c0 = lane * K, cells_row = (U1 + K - 1) / K * K;
+    const int chain = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c0 = (chain * 64 + lane) * K, cells_row = (U1 + K - 1) / K * K;
     const int coff = min(c0, cells_row - K);  // lanes past the row read its last cells
     const bool keep = (ALPHA || CELLS) && c0 <= Ub;
     double m[K];
@@ -626,19 +751,79 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
         }
       }
     };
+    // Several chain waves: every lane has cells of its own in a ring row (rs = 64 K NW) and writes
+    // them, and only an utterance's last chunk asks whether a row is one of its own: no branch or
+    // mask in a step.  left: the cell to the left of lane 0's, as the wave before left it (wave 0:
+    // the unreachable cell behind the ring).
+    int base = 0;  // ring cell of the next row
+    const int left0 = chain > 0 ? chain * 64 * K - 1 : ring * rs;
+    double2 la[G], lc[G];
+    auto fetch_row = [&](double2(&x)[G][K], double2(&left)[G], int(&xs)[G]) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        xs[g] = base;
+#pragma unroll
+        for (int k = 0; k < K; ++k) x[g][k] = cells[base + c0 + k];
+        left[g] = cells[(chain > 0 ? base : 0) + left0];
+        base += rs;
+        if (base == ring * rs) base = 0;
+      }
+    };
+    auto step_rows = [&](auto last_c, const double2(&x)[G][K], const double2(&left)[G], const int(&xs)[G]) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (decltype(last_c)::value && row + g >= Tb) break;
+        double lm = from_left(m[K - 1], left[g].x);
+        int le = from_left(e[K - 1], (int)(unsigned)(unsigned long long)__double_as_longlong(left[g].y));
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const double om = m[k];
+          const int oe = e[k];
+          cells[xs[g] + c0 + k] = make_double2(om, __longlong_as_double((long long)(unsigned)oe));
+          const int top = max(oe, le);
+          double v = scaled(KIND == 2 ? om : om * x[g][k].x, max(oe - top, -kMaxShift)) +
+                     scaled(lm * x[g][k].y, max(le - top, -kMaxShift));
+          if (KIND == 2) v *= x[g][k].x;
+          const unsigned hi = hi_word(v);
+          m[k] = with_hi(v, (hi & 0x000fffffu) | (1022u << 20));
+          e[k] = top + (int)(hi >> 20) - 1022;
+          lm = om;
+          le = oe;
+        }
+      }
+      row += G;
+    };
+    auto chunk = [&](auto last_c) {
+      fetch_row(pa, la, sa);
+      for (int g0 = 0; g0 < R; g0 += 2 * G) {
+        fetch_row(pb, lc, sb);
+        step_rows(last_c, pa, la, sa);
+        if (g0 + 2 * G < R) fetch_row(pa, la, sa);
+        step_rows(last_c, pb, lc, sb);
+      }
+    };
+    if (NW > 1 && tid == 0) cells[ring * rs] = make_double2(0.5, __longlong_as_double((long long)(unsigned)kZeroExp));
     lds_barrier();
     for (int c = 0; c < end_chunk; ++c) {
       if (seen(c)) end_chunk = c;  // (this chunk's work is harmless)
-      fetch(pa, sa);
-      for (int g0 = 0; g0 < R; g0 += 2 * G) {
-        fetch(pb, sb);
-        steps(pa, sa);
-        if (g0 + 2 * G < R) fetch(pa, sa);
-        steps(pb, sb);
+      if constexpr (NW == 1) {
+        fetch(pa, sa);
+        for (int g0 = 0; g0 < R; g0 += 2 * G) {
+          fetch(pb, sb);
+          steps(pa, sa);
+          if (g0 + 2 * G < R) fetch(pa, sa);
+          steps(pb, sb);
+        }
+      } else {
+        const int mine = c - chain;  // this wave's chunk
+        if (mine >= 0 && mine < nchunks) {
+          if ((mine + 1) * R <= Tb) chunk(std::false_type());
+          else chunk(std::true_type());
+        }
       }
       lds_barrier();
     }
-    if (lane == Ub / K && !(s_bad[0] | s_bad[1])) {
+    if (chain * 64 + lane == Ub / K && !(s_bad[0] | s_bad[1])) {
       double mine = 0.5;
       int exp2 = kZeroExp;
 #pragma unroll
@@ -673,7 +858,7 @@ __global__ __launch_bounds__(kRingThreads, K <= 4 || (K == 8 && KIND != 0) ? 4 :
 }
 
 struct RingPlan {
-  int K, R, ring, rs;  // K = 0: the ring does not fit
+  int K, R, ring, rs, NW;  // K = 0: the ring does not fit
   size_t lds;
 };
 
@@ -683,7 +868,7 @@ struct RingPlan {
 // barriers).  More utterances than compute units: half the LDS, so that two workgroups
 // share one.
 RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
-  const RingPlan none{0, 0, 0, 0, 0};
+  const RingPlan none{0, 0, 0, 0, 1, 0};
   const int U1 = U + 1;
   if (T + U > kRingMaxSteps) return none;
   int K0 = 1;
@@ -700,7 +885,7 @@ RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
         const int ring = round_up(lag + (alpha ? 3 : 2) * R, R);
         const size_t lds = (size_t)ring * rs * sizeof(double2);
         if (R * U1 <= kRingLoads * kRingWorkers && lds <= (half ? kRingLds / 2 : kRingLds)) {
-          return RingPlan{K, R, ring, rs, lds};
+          return RingPlan{K, R, ring, rs, 1, lds};
         }
       }
       if (kind != 0) break;  // no lag: more cells per lane save nothing
@@ -708,18 +893,37 @@ RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
   return none;
 }
 
-template <int K, int KIND, int MODE>
+// The same with several chain waves, for eq. (2) and (3): a workgroup per CU at most, and the
+// smallest step whose ring fits.
+RingPlan plan_chain_waves(int groups, int T, int U, int ncu) {
+  const int U1 = U + 1;
+  if (groups <= std::min(ncu, 256) && T + U <= kRingMaxSteps)
+    for (int K = 1; K <= 4; K *= 2) {
+      const int NW = (U1 + 64 * K - 1) / (64 * K), rs = 64 * K * NW;
+      if (NW < 2) break;
+      if (NW > (K == 1 ? 3 : 2)) continue;
+      for (int R = 16; R >= 2 * (K <= 2 ? 4 : 2); R /= 2) {
+        const int ring = (NW + 2) * R;
+        const size_t lds = ((size_t)ring * rs + 1) * sizeof(double2);
+        if (R * U1 <= kRingLoads * (kRingThreads - 64 * NW) && lds <= kRingLds)
+          return RingPlan{K, R, ring, rs, NW, lds};
+      }
+    }
+  return RingPlan{0, 0, 0, 0, 1, 0};
+}
+
+template <int K, int KIND, int MODE, int NW = 1>
 hipError_t launch_ring_t(const RingPlan& p, const float* blank, const float* label,
                          const int* lengths, int B, int T, int U, double* total, float* alpha,
-                         int* status, int2* cells, int2* zcell, hipStream_t st) {
+                         int* status, int2* cells, int2* zcell, const double* probs, hipStream_t st) {
   static LdsGrant grant;
   if (p.lds > 65536) {
-    const hipError_t e = grant((const void*)k_transducer_ring<K, KIND, MODE>, p.lds);
+    const hipError_t e = grant((const void*)k_transducer_ring<K, KIND, MODE, NW>, p.lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_transducer_ring<K, KIND, MODE>), dim3(MODE == kCells ? 2 * B : B), dim3(kRingThreads),
-                     p.lds, st, blank, label, lengths, T, U, total, alpha, status, cells, zcell, p.R, p.ring,
-                     p.rs);
+  hipLaunchKernelGGL((k_transducer_ring<K, KIND, MODE, NW>), dim3(MODE == kCells ? 2 * B : B), dim3(kRingThreads),
+                     p.lds, st, blank, label, lengths, T, U, total, alpha, status, cells, zcell, probs, p.R,
+                     p.ring, p.rs);
   return hipGetLastError();
 }
 
@@ -728,9 +932,9 @@ hipError_t launch_ring(const RingPlan& p, const float* blank, const float* label
                        const int* lengths, int B, int T, int U, double* total, float* alpha,
                        int* status, hipStream_t st) {
   return alpha ? launch_ring_t<K, KIND, kAlpha>(p, blank, label, lengths, B, T, U, total, alpha, status, nullptr,
-                                                nullptr, st)
+                                                nullptr, nullptr, st)
                : launch_ring_t<K, KIND, kTotals>(p, blank, label, lengths, B, T, U, total, nullptr, status,
-                                                 nullptr, nullptr, st);
+                                                 nullptr, nullptr, nullptr, st);
 }
 
 template <int KIND>
@@ -813,41 +1017,61 @@ __global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank,
     rz *= exp_parts(bl[(size_t)(Tb - 1) * U1 + Ub], k);
     ez -= k;
   }
-  // cells in turns of kShareCells; (t, u) of the next cell without a division
+  // Cells in turns of kShareCells, Q a thread: (t, u) of the next without a division, and what all
+  // of them need asked for before any is used (cells that need nothing read the first).
+  constexpr int Q = kShareCells / 256;
   const int dt = 256 / U1, du = 256 - dt * U1;
+  const float* lbs = U > 0 ? lb : bl;
   for (long long from = (long long)part * kShareCells; from < n; from += (long long)parts * kShareCells) {
-    long long at = from + threadIdx.x;
-    int t = (int)(at / U1), u = (int)(at - (long long)t * U1);
+    const long long at0 = from + threadIdx.x;
+    int t = (int)(at0 / U1), u = (int)(at0 - (long long)t * U1);
+    int ts[Q], us[Q];
+    bool in[Q], lab[Q], on[Q];      // inside the utterance; with a label; (eq. 3) with one before
+    int2 ca0[Q], ca1[Q], cb0[Q], cb1[Q];
+    float xb[Q], xl[Q], xp[Q];
 #pragma unroll
-    for (int q = 0; q < kShareCells / 256; ++q, at += 256, t += dt, u += du) {
+    for (int q = 0; q < Q; ++q, t += dt, u += du) {
       if (u >= U1) {
         u -= U1;
         ++t;
       }
-      if (at >= n) break;
+      ts[q] = t;
+      us[q] = u;
+      const long long at = at0 + 256 * q;
+      in[q] = live && at < n && t < Tb && u <= Ub;
+      lab[q] = in[q] && u < Ub;
+      on[q] = KIND == 2 && in[q] && u > 0;
+      const long long row = (long long)(Tb - 1 - t) * U1 + (Ub - u);  // the same frame and label, from the end
+      ca0[q] = ca[in[q] ? at : 0];
+      if (KIND == 2) ca1[q] = ca[on[q] ? at - 1 : 0];
+      cb0[q] = cb[in[q] && (KIND != 0 || t < Tb - 1) ? (KIND == 0 ? row - U1 : row) : 0];
+      cb1[q] = cb[lab[q] ? row - 1 : 0];
+      if (KIND != 2) xb[q] = bl[in[q] ? at : 0];
+      xl[q] = lbs[lab[q] ? (long long)t * U + u : 0];
+      if (KIND == 2) xp[q] = lbs[on[q] ? (long long)t * U + u - 1 : 0];
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const long long at = at0 + 256 * q;
       float sb = 0.f, sl = 0.f;
-      if (live && t < Tb && u <= Ub) {
-        const int2 a = ca[at];
-        const int2* row = cb + (size_t)(Tb - 1 - t) * U1 + (Ub - u);  // the same frame and label
-        const bool lab = u < Ub;
-        const float xl = lab ? lb[(size_t)t * U + u] : 0.f;
-        if (KIND == 0) {
-          const bool last = t == Tb - 1;
-          if (last) sb = u == Ub ? 1.f : 0.f;
-          else sb = share(a, bl[at], row[-(ptrdiff_t)U1], rz, ez);
-        } else if (KIND == 1) {
-          sb = share(a, bl[at], row[0], rz, ez);
+      if (in[q]) {
+        if (KIND == 2) {
+          sb = share(ca0[q], 0.f, cb0[q], rz, ez);
+          if (on[q]) sb += share(ca1[q], xp[q], cb0[q], rz, ez);
+        } else if (KIND == 0 && ts[q] == Tb - 1) {
+          sb = us[q] == Ub ? 1.f : 0.f;
         } else {
-          sb = share(a, 0.f, row[0], rz, ez);
-          if (u > 0) sb += share(ca[at - 1], lb[(size_t)t * U + u - 1], row[0], rz, ez);
+          sb = share(ca0[q], xb[q], cb0[q], rz, ez);
         }
-        if (lab) sl = share(a, xl, row[-1], rz, ez);
+        if (lab[q]) sl = share(ca0[q], xl[q], cb1[q], rz, ez);
         if (bad) sb = sl = NAN;
         sb = (float)(w * (double)sb);
         sl = (float)(w * (double)sl);
       }
-      gb[at] = sb;
-      if (u < U) gl[(size_t)t * U + u] = sl;
+      if (at < n) {
+        gb[at] = sb;
+        if (us[q] < U) gl[(size_t)ts[q] * U + us[q]] = sl;
+      }
     }
   }
 }
@@ -856,23 +1080,48 @@ template <int KIND>
 hipError_t launch_gradient(const float* blank, const float* label, const int* lengths, const double* weights, int B,
                            int T, int U, double* total, float* grad_blank, float* grad_label, int* status,
                            int2* cells, int2* zcell, hipStream_t st) {
-  const RingPlan p = plan_ring(KIND, 2 * B, T, U, true, device_cus());
-  auto ring = [&](auto k) {
-    return launch_ring_t<decltype(k)::value, KIND, kCells>(p, blank, label, lengths, B, T, U, total, nullptr, status,
-                                                           cells, zcell, st);
+  double* probs = reinterpret_cast<double*>(zcell + transducer_zcells(B));
+  RingPlan p = KIND == 0 ? RingPlan{} : plan_chain_waves(2 * B, T, U, device_cus());
+  if (p.K == 0) p = plan_ring(KIND, 2 * B, T, U, true, device_cus());
+  auto ring = [&](auto k, auto nw) {
+    return launch_ring_t<decltype(k)::value, KIND, kCells, decltype(nw)::value>(
+        p, blank, label, lengths, B, T, U, total, nullptr, status, cells, zcell, probs, st);
   };
+  using std::integral_constant;
+  integral_constant<int, 1> one;
+  integral_constant<int, 2> two;
+  integral_constant<int, 4> four;
   hipError_t e = hipSuccess;
+  if (ring_takes_probs(p.K, p.NW)) {
+    hipLaunchKernelGGL(k_probs, dim3(B * kProbParts), dim3(256), 0, st, blank, label, lengths, B, T, U, probs);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   switch (p.K) {
     case 0:
       hipLaunchKernelGGL(k_scores_logs<KIND>, dim3(2 * B), dim3(kRingThreads), 0, st, blank, label, lengths, T, U,
                          total, status, cells, zcell);
       e = hipGetLastError();
       break;
-    case 1: e = ring(std::integral_constant<int, 1>()); break;
-    case 2: e = ring(std::integral_constant<int, 2>()); break;
-    case 4: e = ring(std::integral_constant<int, 4>()); break;
-    case 8: e = ring(std::integral_constant<int, 8>()); break;
-    default: e = ring(std::integral_constant<int, 16>());
+    case 1:
+      if (p.NW == 1) e = ring(one, one);
+      if constexpr (KIND != 0) {
+        if (p.NW == 2) e = ring(one, two);
+        if (p.NW == 3) e = ring(one, integral_constant<int, 3>());
+      }
+      break;
+    case 2:
+      if (p.NW == 1) e = ring(two, one);
+      if constexpr (KIND != 0)
+        if (p.NW == 2) e = ring(two, two);
+      break;
+    case 4:
+      if (p.NW == 1) e = ring(four, one);
+      if constexpr (KIND != 0)
+        if (p.NW == 2) e = ring(four, two);
+      break;
+    case 8: e = ring(integral_constant<int, 8>(), one); break;
+    default: e = ring(integral_constant<int, 16>(), one);
   }
   if (e != hipSuccess) return e;
   const long long n = (long long)T * (U + 1);

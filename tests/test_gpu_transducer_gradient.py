@@ -123,6 +123,20 @@ def test_wide_and_many_standard(B, T, U):
     _check("standard", blank, label, frames, labels)
 
 
+@pytest.mark.parametrize("kind", ["modified", "constrained"])
+@pytest.mark.parametrize("T,U", [(70, 64), (90, 65), (130, 127), (129, 128), (210, 190), (230, 192), (250, 200),
+                                 (260, 206), (270, 207), (300, 255), (500, 470), (530, 511), (520, 512)])
+def test_chain_splits(kind, T, U):
+    """Few utterances: one to four waves side by side, one to sixteen cells a lane; ragged ones
+    whose labels end inside any wave, and inputs that the linear domain does not take."""
+    blank, label, frames, labels = _inputs(T + U, 4, T, U)
+    labels = np.minimum(labels, frames)
+    labels[1] = min(63, frames[1])
+    blank[2, frames[2] // 2, labels[2] // 2] = -np.inf
+    label[3, :, labels[3] // 2] = -400.0
+    _check(kind, blank, label, frames, labels)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_likely_paths_and_weights(kind):
     """Inputs as a trained model gives them (a few cells carry the path, the rest are steep),
