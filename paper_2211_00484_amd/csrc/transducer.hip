@@ -568,39 +568,52 @@ __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND 
     }
     auto request = [&](auto set, int i0) {
       constexpr int d = decltype(set)::value;
-      if (D > 1) read[d] = 0;
-      const In *gb, *gl, *any;
-      if constexpr (!PROBS) {
-        gb = any = bl;
-        gl = lb;
-      } else {
-        gb = any = pbl;
-        gl = plb;
-      }
       const int left = Tb - i0;
-      int bleft = left;
-      if (rev) {  // rows and cells counted from the end: element j lies j before these
-        gb += (ptrdiff_t)(blank_row<KIND, true>(i0, Tb)) * U1 + Ub;
-        gl += (ptrdiff_t)(Tb - 1 - i0) * U + Ub - 1;
-        if (KIND == 2) bleft = left - 1;
-      } else {
-        gb += (ptrdiff_t)(i0 - 1 + kOut) * U1;
-        gl += (ptrdiff_t)i0 * U;
-      }
+      if constexpr (!CELLS) {
+        const float* gb = bl + (ptrdiff_t)(i0 - 1 + kOut) * U1;
+        const float* gl = lb + (ptrdiff_t)i0 * U;
 #pragma unroll
-      for (int q = 0; q < L; ++q) {
-        const int j = rev ? -(w + q * W) : w + q * W;
-        const bool rb = bcell[q] >= 0 && brow[q] < bleft && (KIND != 0 || i0 + brow[q] > 0);
-        const bool rl = lcell[q] >= 0 && lrow[q] < left;
-        if (D > 1) {
-          xb[d][q] = *(rb ? gb + j : any);
-          xl[d][q] = *(rl ? gl + j : any);
-          read[d] |= (rb ? 1u : 0u) << (2 * q) | (rl ? 2u : 0u) << (2 * q);
-        } else {
+        for (int q = 0; q < L; ++q) {
           xb[d][q] = 0.f;
           xl[d][q] = 0.f;
-          if (rb) xb[d][q] = gb[j];
-          if (rl) xl[d][q] = gl[j];
+          if (bcell[q] >= 0 && brow[q] < left && (KIND != 0 || i0 + brow[q] > 0))
+            xb[d][q] = gb[w + q * W];
+          if (lcell[q] >= 0 && lrow[q] < left) xl[d][q] = gl[w + q * W];
+        }
+      } else {
+        const In *gb, *gl, *any;
+        if constexpr (!PROBS) {
+          gb = any = bl;
+          gl = lb;
+        } else {
+          gb = any = pbl;
+          gl = plb;
+        }
+        int bleft = left;
+        if (rev) {  // rows and cells counted from the end: element j lies j before these
+          gb += (ptrdiff_t)(blank_row<KIND, true>(i0, Tb)) * U1 + Ub;
+          gl += (ptrdiff_t)(Tb - 1 - i0) * U + Ub - 1;
+          if (KIND == 2) bleft = left - 1;
+        } else {
+          gb += (ptrdiff_t)(i0 - 1 + kOut) * U1;
+          gl += (ptrdiff_t)i0 * U;
+        }
+        if (D > 1) read[d] = 0;
+#pragma unroll
+        for (int q = 0; q < L; ++q) {
+          const int j = rev ? -(w + q * W) : w + q * W;
+          const bool rb = bcell[q] >= 0 && brow[q] < bleft && (KIND != 0 || i0 + brow[q] > 0);
+          const bool rl = lcell[q] >= 0 && lrow[q] < left;
+          if (D > 1) {
+            xb[d][q] = *(rb ? gb + j : any);
+            xl[d][q] = *(rl ? gl + j : any);
+            read[d] |= (rb ? 1u : 0u) << (2 * q) | (rl ? 2u : 0u) << (2 * q);
+          } else {
+            xb[d][q] = 0.f;
+            xl[d][q] = 0.f;
+            if (rb) xb[d][q] = gb[j];
+            if (rl) xl[d][q] = gl[j];
+          }
         }
       }
     };
@@ -619,15 +632,17 @@ __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND 
 #pragma unroll
       for (int q = 0; q < L; ++q) {
         if constexpr (!PROBS) {
-          const float vb = D == 1 || (read[d] >> (2 * q) & 1) ? xb[d][q] : 0.f;
-          const float vl = D == 1 || (read[d] >> (2 * q) & 2) ? xl[d][q] : 0.f;
+          if constexpr (D > 1) {
+            if (!(read[d] >> (2 * q) & 1)) xb[d][q] = 0.f;
+            if (!(read[d] >> (2 * q) & 2)) xl[d][q] = 0.f;
+          }
           if (bcell[q] >= 0) {
-            note(vb);
-            reinterpret_cast<double*>(cells + c0 + bcell[q])[0] = exp_log_prob(vb);
+            note(xb[d][q]);
+            reinterpret_cast<double*>(cells + c0 + bcell[q])[0] = exp_log_prob(xb[d][q]);
           }
           if (lcell[q] >= 0) {
-            note(vl);
-            reinterpret_cast<double*>(cells + c0 + lcell[q])[1] = exp_log_prob(vl);
+            note(xl[d][q]);
+            reinterpret_cast<double*>(cells + c0 + lcell[q])[1] = exp_log_prob(xl[d][q]);
           }
         } else {
           if (bcell[q] >= 0)
@@ -646,38 +661,44 @@ __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND 
     if (ALPHA && KIND != 0)  // alpha row 0
       for (int u = w; u < U1; u += W) (al - U1)[u] = u == 0 ? 0.f : -INFINITY;
     produce(set0);
-    // chunk c + 1 lies in set c % D when iteration c begins
-    auto ahead = [&](auto set, int c) {
-      if (D == 1 || c < nchunks) request(set, c * R);
-    };
-    int s0 = 0;  // ring cell of the next chunk to store
-    auto store_chunk = [&](int c) {  // (as store_rows, by the elements' places)
-      if (c < 0) return;
-      int2* to = mine_cells + (size_t)c * R * U1;
-      const int left = Tb - c * R;
-#pragma unroll
-      for (int q = 0; q < L; ++q)
-        if (bcell[q] >= 0 && brow[q] < left) {
-          const double2 x = cells[s0 + bcell[q]];
-          to[w + q * W] = make_int2(__float_as_int((float)x.x),
-                                    (int)(unsigned)(unsigned long long)__double_as_longlong(x.y));
-        }
-      s0 += R * rs;
-      if (s0 == ring * rs) s0 = 0;
-    };
-    auto turn = [&](auto set, int c) {
-      if (seen(c)) end_chunk = c;  // (this chunk's work is harmless)
-      if (c + 1 < nchunks) produce(set);
-      if (c + 1 + D < nchunks) request(set, (c + 1 + D) * R);
-      if constexpr (NW > 1) store_chunk(c - NW);
-      else if (ALPHA || CELLS) store_rows((c - 1) * R - lag, c * R - lag, w, W);
-      if (highest > __float_as_int(kRingMaxLog) || lowest > __float_as_uint(kRingMinLog)) s_bad[c / 4 & 1] = 1;
+    if constexpr (NW == 1) {
+      request(set0, R);
       lds_barrier();
-    };
-    ahead(set0, 1);
-    if constexpr (D > 1) {
+      for (int c = 0; c < end_chunk; ++c) {
+        if (seen(c)) end_chunk = c;  // (this chunk's work is harmless)
+        if (c + 1 < nchunks) produce(set0);
+        if (c + 2 < nchunks) request(set0, (c + 2) * R);
+        if (ALPHA || CELLS) store_rows((c - 1) * R - lag, c * R - lag, w, W);
+        if (highest > __float_as_int(kRingMaxLog) || lowest > __float_as_uint(kRingMinLog)) s_bad[c / 4 & 1] = 1;
+        lds_barrier();
+      }
+    } else {  // chunk c + 1 lies in set c % D when iteration c begins
+      int s0 = 0;  // ring cell of the next chunk to store
+      auto store_chunk = [&](int c) {  // (as store_rows, by the elements' places)
+        if (c < 0) return;
+        int2* to = mine_cells + (size_t)c * R * U1;
+        const int left = Tb - c * R;
+#pragma unroll
+        for (int q = 0; q < L; ++q)
+          if (bcell[q] >= 0 && brow[q] < left) {
+            const double2 x = cells[s0 + bcell[q]];
+            to[w + q * W] = make_int2(__float_as_int((float)x.x),
+                                      (int)(unsigned)(unsigned long long)__double_as_longlong(x.y));
+          }
+        s0 += R * rs;
+        if (s0 == ring * rs) s0 = 0;
+      };
+      auto turn = [&](auto set, int c) {
+        if (seen(c)) end_chunk = c;
+        if (c + 1 < nchunks) produce(set);
+        if (c + 1 + D < nchunks) request(set, (c + 1 + D) * R);
+        store_chunk(c - NW);
+        if (highest > __float_as_int(kRingMaxLog) || lowest > __float_as_uint(kRingMinLog)) s_bad[c / 4 & 1] = 1;
+        lds_barrier();
+      };
       std::integral_constant<int, 1> set1;
-      ahead(set1, 2);
+      if (1 < nchunks) request(set0, R);
+      if (2 < nchunks) request(set1, 2 * R);
       lds_barrier();
       for (int c = 0; c < end_chunk;) {
         turn(set0, c);
@@ -685,9 +706,6 @@ __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND 
         turn(set1, c);
         ++c;
       }
-    } else {
-      lds_barrier();
-      for (int c = 0; c < end_chunk; ++c) turn(set0, c);
     }
   } else {
     __builtin_amdgcn_s_setprio(3);  // the other waves have slack
