@@ -422,8 +422,8 @@ tbs_status tbs_transducer_forward(int32_t kind, const float *blank, const float 
  *   workspace       DEVICE, 16-byte aligned, of at least the bytes that
  *                   tbs_transducer_gradient_workspace gives for B, T and U; contents on
  *                   entry are of no matter.  Calls that may overlap need one each.
- * Errors: as tbs_transducer_forward; TBS_EINVAL for a workspace that is too small or not
- * aligned.
+ * Errors: as tbs_transducer_forward; TBS_ECAPACITY for B > 2^21 or T > 2^30; TBS_EINVAL for a
+ * workspace that is too small or not aligned.
  */
 size_t tbs_transducer_gradient_workspace(int32_t B, int32_t T, int32_t U);
 tbs_status tbs_transducer_gradient(int32_t kind, const float *blank, const float *label,
@@ -521,10 +521,12 @@ tbs_status tbs_linear_backward(int32_t dtype, const void *grad_out, int64_t ldg,
  *                  a state outside the graph (-1, say) leaves its row without this mask.
  *                  Both or neither NULL;
  *   workspace      DEVICE, 16-byte aligned, of at least tbs_adjust_logits_workspace bytes
- *                  (0: none, may be NULL); calls that may overlap need one each.
+ *                  (0: none, may be NULL; none without normalize); calls that may overlap
+ *                  need one each.
  * R >= 0 (0 is a no-op).  Errors: TBS_EINVAL for an unknown dtype, sizes, NULL pointers, row
  * lengths below the width, penalties out of range, a graph of another vocabulary or a
- * workspace that is too small; TBS_ECAPACITY for R * V too large for a launch.
+ * workspace that is too small; TBS_ECAPACITY for V > 2^30 or more rows than
+ * a launch takes (some 2^23 workgroups, of up to 8,192 labels each).
  */
 typedef struct {
   const int32_t *history;

@@ -6,8 +6,10 @@
 // registers (16 bytes a lane and access); meanwhile the counts of the row's history and the
 // bits of its state's arcs are gathered in LDS, from which each lane takes its columns'.  The
 // history and the arcs are read again by each workgroup of a row, for the columns of its own.
-// Bound: memory (a logit is read and written once), and for few rows latency: state, arc
-// range, arcs, and the history are dependent round trips.  A log-softmax over more columns than a
+// Bound: memory (a logit is read and written once; MI355X, 2,048 x 5,000 fp32 with a history of 120,
+// a graph and the log-softmax 22 us, 3.8 TB/s), the scan of long histories (512 x 46,340 bf16
+// with 2,000 labels each 38 us, 2.6 TB/s), and for few rows latency: state, arc range, arcs, and
+// the history are dependent round trips (128 x 500 4.6 us).  A log-softmax over more columns than a
 // workgroup holds takes two passes: sums first, then everything again with the row's
 // normaliser.
 #include <hip/hip_runtime.h>
@@ -101,11 +103,22 @@ __global__ __launch_bounds__(kThreads) void k_adjust(AdjustArgs p) {
         *reinterpret_cast<int4*>(count + 4 * (q * kThreads + tid)) = make_int4(0, 0, 0, 0);
     for (int i = tid; i < W / 32; i += kThreads) arcs[i] = 0;
     __syncthreads();
-    for (int i = tid; i < len; i += kThreads) {
-      const unsigned c = (unsigned)hist[i] - (unsigned)c0;
-      if (hist[i] >= 0 && c < (unsigned)n) atomicAdd(&count[c], 1);
+    for (unsigned i = 4 * tid; i < (unsigned)len; i += 4 * kThreads) {
+      Vec<int, 4> h = {{-1, -1, -1, -1}};
+      if (i + 4 <= (unsigned)len) {
+        h = load_vec<int, 4>(hist + i);
+      } else {
+#pragma unroll
+        for (unsigned k = 0; k < 4; ++k)
+          if (i + k < (unsigned)len) h.v[k] = hist[i + k];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned c = (unsigned)h.v[k] - (unsigned)c0;
+        if (h.v[k] >= 0 && c < (unsigned)n) atomicAdd(&count[c], 1);
+      }
     }
-    for (int i = lo + tid; i < hi; i += kThreads) {
+    for (unsigned i = (unsigned)lo + tid; i < (unsigned)hi; i += kThreads) {
       const unsigned c = (unsigned)p.graph_label[i] - (unsigned)c0;
       if (c < (unsigned)n) atomicOr(&arcs[c / 32], 1u << (c % 32));
     }
@@ -224,6 +237,7 @@ hipError_t launch_t(const AdjustArgs& p, hipStream_t st) {
 // Columns per workgroup: the whole row where a workgroup holds it and a log-softmax wants it
 // (one pass); else as many as leave two workgroups per CU, since each reads the history again.
 bool plan_adjust(AdjustArgs& p, int dtype) {
+  if (p.V > 1 << 30) return false;
   const int one = (dtype == kF32 ? 4 : 8) * kThreads;
   const int cus = device_cus() > 0 ? device_cus() : 256;
   auto parts = [&](int per) { return (p.V - 1) / per + 1; };

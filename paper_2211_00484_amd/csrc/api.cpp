@@ -1975,6 +1975,7 @@ tbs_status tbs_transducer_gradient(int32_t kind, const float* blank, const float
   if (U + 1 > 64 * kTransducerMaxK)
     return fail(TBS_ECAPACITY, "%s: U = %d exceeds the limit %d", who, (int)U, 64 * kTransducerMaxK - 1);
   if (B > 1 << 21) return fail(TBS_ECAPACITY, "%s: B = %d exceeds the limit %d", who, (int)B, 1 << 21);
+  if (T > 1 << 30) return fail(TBS_ECAPACITY, "%s: T = %d exceeds the limit %d", who, (int)T, 1 << 30);
   if (B == 0) return TBS_OK;
   if (!blank || (U > 0 && !label) || !lengths || !out_total || !out_grad_blank ||
       (U > 0 && !out_grad_label))
@@ -2127,6 +2128,7 @@ tbs_status tbs_adjust_logits(int32_t dtype, const void* logits, int64_t ld_logit
   const char* who = "tbs_adjust_logits";
   if (!known_dtype(dtype)) return fail(TBS_EINVAL, "%s: unknown dtype %d", who, dtype);
   if (R < 0 || V < 1) return fail(TBS_EINVAL, "%s: need R >= 0, V >= 1", who);
+  if (V > 1 << 30) return fail(TBS_ECAPACITY, "%s: V = %d exceeds the limit %d", who, V, 1 << 30);
   if (!adjustments) return fail(TBS_EINVAL, "%s: adjustments is NULL", who);
   const tbs_adjustments& a = *adjustments;
   if (a.history && (a.history_cols < 0 || a.ld_history < a.history_cols))

@@ -5,6 +5,16 @@
 // stored with k along its rows (KC: x and W of the forward product, dz of dx) or with k down
 // its columns (W of dx, both operands of dW).  Sums are fp32 on the matrix units: bf16 and
 // fp16 operands by 16x16x32 products, fp32 operands by 16x16x4 products.
+//
+// dz is rounded to the element type before dx and dW, as a matrix instruction takes it: their
+// errors against 64 bits are then those of two roundings (1.4 times those of one).
+//
+// Bound, MI355X: 16-bit, the matrix units (in the main loop of 128 x 128 tiles they are busy 86%
+// of its cycles, of 256 x 256 tiles 70%) and, for K of a few hundred, what is not the main loop:
+// 64,000 x 512, K = 2,048 fp16 with a residual 150 us, 895 TFLOP/s (the library's product alone
+// 111); 6,000 x 5,000, K = 512 bf16 47 us, 650 TFLOP/s (76).  At K = 512 a 256 x 256 tile's main loop
+// takes 14 us and its results 6, written at 5.6 TB/s while every CU writes.  fp32: the fp32 matrix
+// instructions, 8,000 x 512, K = 384 33 us (32), 8,192 x 2,048, K = 2,048 138 TFLOP/s (137).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -136,7 +146,7 @@ __device__ __forceinline__ Vec<T, E> load_residual(const LinearEpilogue& e, int 
 
 // ---------------------------------------------------------------------------
 // staging of an operand's slice: ROWS rows (m or n) x 128 bytes of k, as 16-byte chunks
-// (128: a whole cache line of each row; slices of 64 bytes halve the rate of the loads)
+// (a whole cache line of each row: 64,000 x 512, K = 2,048 fp16 165 us, 197 in slices of 64 bytes)
 
 template <class T>
 constexpr int kChunkElems = 16 / (int)sizeof(T);
@@ -165,11 +175,10 @@ __device__ __forceinline__ uint4 load_chunk_guarded(const T* row, int k, int n) 
   return v;
 }
 
-// Places of a slice's chunks in LDS, numbered in the order in which direct copies fill them:
-// 64 in a row by a wave, 16 bytes a lane, lanes in a row taking pieces of a cache line in a row
-// (the loads take four times as long where the lanes permute them: 148 M single accesses
-// for 134 M chunks).  So conflicts are kept off not by permuting chunks but by sharing the rows
-// out to blocks, a pad behind each:
+// Places of a slice's chunks in LDS, numbered in the order in which direct copies fill them: 64 in
+// a row by a wave, 16 bytes a lane.  Bank conflicts are kept off by sharing the rows out to blocks
+// with a pad behind each, so that a fragment's address is its lane's constant plus constants
+// (permuting the chunks of a row instead measured the same):
 //  - KC: row r to block r % 8, pads of 16 bytes: 8 rows of a fragment meet 8 places;
 //  - not KC, 16-bit: k row r to block r % 4, pads of 32: a transposing read's 4 k rows x 32 bytes;
 //  - not KC, fp32: k row r to block r / 4 % 4, pads of 64: rows of two lane groups x 64 bytes.
@@ -655,7 +664,7 @@ __global__ __launch_bounds__(256) void k_join_parts(ProductArgs p) {
   }
 }
 
-// dz = dy act'(pre), four elements per thread
+// dz = dy act'(pre), 16 bytes a thread and turn.  Bound: memory (8,000 x 512 fp32 10.4 us, 4.7 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void k_act_grad(const T* __restrict__ dy, long long ldy, const T* __restrict__ pre,
                                                   long long ldp, T* __restrict__ dz, long long ldz, int M, int N,
@@ -779,10 +788,12 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   p.tiles_n = (p.N + bn[p.shape] - 1) / bn[p.shape];
   const long long n = tiles(p.shape);
   long long splits = 1;
-  // Fewer tiles than CUs: k in parts of 8 slices at least, two workgroups per CU (dW of 500 x 512
-  // over 40,000 rows: 41 us in 32 parts, 66 in 8; shorter parts do not pay for the join: 512 x
-  // 512, K = 512, 15.5 us whole, 19 in 2).
-  if (n < cus) splits = std::max(1ll, std::min((2 * cus + n - 1) / n, (long long)slices / 8));
+  // Fewer tiles than CUs: k in parts of 8 slices at least, as many as the CUs hold at once (three
+  // workgroups of 64 x 64 tiles each, two of 128 x 128): dW of 512 x 384 fp32 over 8,000 rows, 48
+  // tiles, 41 us in 16 parts, 51 in 11, whose CUs have two or three; of 500 x 512 bf16 over 40,000,
+  // 16 tiles, 41 in 32, 66 in 8.  Shorter parts do not pay for the join (512 x 512, K = 512 bf16
+  // 15.5 us whole, 19 in 2).
+  if (n < cus) splits = std::max(1ll, std::min((p.shape == 0 ? 3 : 2) * cus / n, (long long)slices / 8));
   p.slices_per = std::max(1, (int)((slices + splits - 1) / splits));
   p.splits = std::max(1, (slices + p.slices_per - 1) / p.slices_per);
   return true;

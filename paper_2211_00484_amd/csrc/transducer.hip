@@ -888,7 +888,7 @@ struct RingPlan {
 RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
   const RingPlan none{0, 0, 0, 0, 1, 0};
   const int U1 = U + 1;
-  if (T + U > kRingMaxSteps) return none;
+  if (T > kRingMaxSteps - U) return none;
   int K0 = 1;
   while (64 * K0 < U1) K0 *= 2;
   for (int half = B > ncu; half >= 0; --half)
@@ -915,7 +915,7 @@ RingPlan plan_ring(int kind, int B, int T, int U, bool alpha, int ncu) {
 // smallest step whose ring fits.
 RingPlan plan_chain_waves(int groups, int T, int U, int ncu) {
   const int U1 = U + 1;
-  if (groups <= std::min(ncu, 256) && T + U <= kRingMaxSteps)
+  if (groups <= std::min(ncu, 256) && T <= kRingMaxSteps - U)
     for (int K = 1; K <= 4; K *= 2) {
       const int NW = (U1 + 64 * K - 1) / (64 * K), rs = 64 * K * NW;
       if (NW < 2) break;

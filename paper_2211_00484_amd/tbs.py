@@ -873,7 +873,7 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
             if R > 0 and o.data_ptr() != out.data_ptr():
                 raise ValueError("out must have contiguous rows at one distance")
         L = lib()
-        nbytes = L.tbs_adjust_logits_workspace(code, R, V, a.normalize)
+        nbytes = L.tbs_adjust_logits_workspace(code, R, V, 1) if normalize else 0
         ws = _workspace(nbytes, logits)
         _check(L.tbs_adjust_logits(code, _ptr(z), ldz, R, V, ctypes.byref(a),
                                    _ptr(out if o is None else o), ldo, _ptr(ws), nbytes,

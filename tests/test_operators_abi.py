@@ -99,6 +99,18 @@ def test_adjust_refusals(change, fragment):
     assert fragment in _message()
 
 
+def test_sizes_beyond_the_limits():
+    assert _adjust(V=2 ** 30 + 1, ldz=2 ** 31, ldo=2 ** 31) == ECAPACITY and "limit" in _message()
+    assert _adjust(R=2 ** 31 - 1, V=2 ** 20, ldz=2 ** 20, ldo=2 ** 20) == ECAPACITY
+    L = tbs.lib()
+    assert L.tbs_transducer_gradient(0, P, P, P, None, 1, 2 ** 30 + 1, 1, P, P, P, None, P, 1 << 62,
+                                     None) == ECAPACITY
+    assert L.tbs_transducer_gradient(0, P, P, P, None, 2 ** 21 + 1, 2, 1, P, P, P, None, P, 1 << 62,
+                                     None) == ECAPACITY
+    big = dict(LINEAR, K=2 ** 30 + 1, ldx=2 ** 31, ldw=2 ** 31)
+    assert L.tbs_linear(*big.values(), None) == ECAPACITY
+
+
 def test_adjust_empty_batch():
     assert _adjust(R=0, logits=None, out=None) == 0
 
