@@ -780,10 +780,12 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   // quarter of a second round, 46.8 against 42.9.  fp32 operands, bound by their matrix
   // instructions, spread best in small tiles: 8,000 x 384, K = 512 31.8 us by 64 x 64, 47.2 by
   // 128 x 128.
+  // A tile no more than twice as wide as the result.
   const long long rounds = (tiles(2) + cus - 1) / cus;
-  if (dtype == kF32) p.shape = tiles(1) >= 4 * cus ? 1 : 0;
-  else if (4 * tiles(2) >= 3 * rounds * cus) p.shape = 2;
-  else p.shape = tiles(1) * slices >= 8 * cus ? 1 : 0;
+  const int least = std::min(p.M, p.N);
+  if (dtype == kF32) p.shape = least > 64 && tiles(1) >= 4 * cus ? 1 : 0;
+  else if (least > 128 && 4 * tiles(2) >= 3 * rounds * cus) p.shape = 2;
+  else p.shape = least > 64 && tiles(1) * slices >= 8 * cus ? 1 : 0;
   p.tiles_m = (p.M + bm[p.shape] - 1) / bm[p.shape];
   p.tiles_n = (p.N + bn[p.shape] - 1) / bn[p.shape];
   const long long n = tiles(p.shape);
@@ -792,8 +794,12 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   // workgroups of 64 x 64 tiles each, two of 128 x 128): dW of 512 x 384 fp32 over 8,000 rows, 48
   // tiles, 41 us in 16 parts, 51 in 11, whose CUs have two or three; of 500 x 512 bf16 over 40,000,
   // 16 tiles, 41 in 32, 66 in 8.  Shorter parts do not pay for the join (512 x 512, K = 512 bf16
-  // 15.5 us whole, 19 in 2).
-  if (n < cus) splits = std::max(1ll, std::min((p.shape == 0 ? 3 : 2) * cus / n, (long long)slices / 8));
+  // 15.5 us whole, 19 in 2), but for fp32, whose slices take longest, down to 4 slices while no CU
+  // has two (369 x 256, K = 512 11.4 us in 2 parts, 9.2 in 4; 935 x 500, K = 640 14.8 in 2, 18.8 in 5).
+  if (n < cus) {
+    splits = std::max(1ll, std::min((p.shape == 0 ? 3 : 2) * cus / n, (long long)slices / 8));
+    if (dtype == kF32) splits = std::max(splits, std::min(cus / n, (long long)slices / 4));
+  }
   p.slices_per = std::max(1, (int)((slices + splits - 1) / splits));
   p.splits = std::max(1, (slices + p.slices_per - 1) / p.slices_per);
   return true;
