@@ -418,24 +418,10 @@ __device__ __forceinline__ double from_left(double v, double fill) {
   return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 
-// steps whose ring cells wave 0 requests together, one group ahead of their use (an LDS
-// read takes longer than a step)
-template <int K>
-constexpr int kRingGroup = K <= 2 ? 4 : K == 4 ? 2 : 1;
-
-// NW > 1 (cells of eq. (2), (3); few utterances, whose time is the chain's): NW chain waves side
-// by side, wave v with cells 64 K v .. and a chunk behind wave v - 1, whose states before each
-// step lie in the ring by then: fewer cells per lane, a shorter step (T = 1,000, U = 150, B = 1:
-// one wave of 4 cells a lane 291 us, three of one cell 147; B = 32, T = 250, U = 80: 44, 29).
-// MODE: kTotals, kAlpha (alpha too), or kCells: the scores of the gradient, one workgroup per
-// utterance and direction (rev: from the end, see above), left as cells.
-// R: rows per chunk (a multiple of 2 kRingGroup<K>; R (U + 1) <= kRingLoads kRingWorkers);
-// ring: rows in LDS, a multiple of R, at least 2 R (with alpha 3 R) plus eq. (1)'s lag of
-// U / K;
-// rs: cells per ring row, at least U + 1 rounded up to K.
-// e^x of every input (T (2 U + 1) per utterance, blank then label) for the ring with several chain
-// waves, whose time on one CU would be its workers' exponentials: T = 1,000, U = 150, B = 1 216 us
-// with them. flags: per part of an utterance, whether an input is none that the ring takes.
+// e^x of every input, blank [B][T][U + 1] then label [B][T][U], for the ring with three chain waves
+// or more cells a lane, whose time on one CU would be its workers' exponentials (T = 1,000, U = 150,
+// B = 1: 216 us with them, 168 by this kernel).  Behind them [B][kProbParts] flags: whether an input
+// of that part of the utterance is none that the ring takes.
 constexpr int kProbParts = kTransducerProbParts;
 constexpr bool ring_takes_probs(int K, int NW) { return NW > 2 || (NW == 2 && K > 1); }
 __global__ __launch_bounds__(256) void k_probs(const float* __restrict__ blank, const float* __restrict__ label,
@@ -464,6 +450,21 @@ __global__ __launch_bounds__(256) void k_probs(const float* __restrict__ blank, 
   if (threadIdx.x == 0) flags[blockIdx.x] = s_flag;
 }
 
+// steps whose ring cells wave 0 requests together, one group ahead of their use (an LDS
+// read takes longer than a step)
+template <int K>
+constexpr int kRingGroup = K <= 2 ? 4 : K == 4 ? 2 : 1;
+
+// NW > 1 (cells of eq. (2), (3); few utterances, whose time is the chain's): NW chain waves side
+// by side, wave v with cells 64 K v .. and a chunk behind wave v - 1, whose states before each
+// step lie in the ring by then: fewer cells per lane, a shorter step (T = 1,000, U = 150, B = 1:
+// one wave of 4 cells a lane 291 us, three of one cell 147; B = 32, T = 250, U = 80: 44, 29).
+// MODE: kTotals, kAlpha (alpha too), or kCells: the scores of the gradient, one workgroup per
+// utterance and direction (rev: from the end, see above), left as cells.
+// R: rows per chunk (a multiple of 2 kRingGroup<K>; R (U + 1) <= kRingLoads times the workers);
+// ring: rows in LDS, a multiple of R, at least 2 R (with alpha 3 R) plus eq. (1)'s lag of
+// U / K; with NW > 1 (NW + 2) R, and one cell behind them;
+// rs: cells per ring row, at least U + 1 rounded up to K; with NW > 1 64 K NW.
 template <int K, int KIND, int MODE, int NW>
 __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND == 0)) ? 2 : 4) void k_transducer_ring(
     const float* __restrict__ blank, const float* __restrict__ label,
