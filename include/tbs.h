@@ -524,8 +524,8 @@ tbs_status tbs_linear_backward(int32_t dtype, const void *grad_out, int64_t ldg,
  *                  (0: none, may be NULL; none without normalize); calls that may overlap
  *                  need one each.
  * R >= 0 (0 is a no-op).  Errors: TBS_EINVAL for an unknown dtype, sizes, NULL pointers, row
- * lengths below the width, penalties out of range, a graph of another vocabulary or a
- * workspace that is too small; TBS_ECAPACITY for V > 2^30 or more rows than
+ * lengths below the width, penalties out of range, a graph of another vocabulary or device or
+ * a workspace that is too small; TBS_ECAPACITY for V > 2^30 or more rows than
  * a launch takes (some 2^23 workgroups, of up to 8,192 labels each).
  */
 typedef struct {

@@ -171,6 +171,7 @@ void lattice_free(tbs_lattice* L);  // release and delete (defined with tbs_latt
 struct tbs_graph {
   int S = 0, start = 0, V = 0, A = 0, maxdeg = 0;
   int trivial = 0;  // one state, 0-weight loops 1..V-1 in label order, final weight 0
+  int dev = 0;      // device of the arrays
   int* rp = nullptr;
   int* dest = nullptr;
   int* label = nullptr;
@@ -777,7 +778,9 @@ tbs_status tbs_graph_create(int32_t num_states, int32_t start_state, int32_t voc
   for (int j = 0; trivial && j < A; ++j)
     trivial = label[j] == j + 1 && dest[j] == 0 && score[j] == 0.f;
   g->trivial = trivial;
-  tbs_status st = graph_upload(g, row_ptr, dest, label, score, final_score);
+  const hipError_t e = hipGetDevice(&g->dev);
+  tbs_status st = e == hipSuccess ? graph_upload(g, row_ptr, dest, label, score, final_score)
+                                  : hip_fail(e, "hipGetDevice");
   if (st != TBS_OK) {
     graph_free(g);
     return st;
@@ -2172,6 +2175,10 @@ tbs_status tbs_adjust_logits(int32_t dtype, const void* logits, int64_t ld_logit
   p.allowed = (const uint32_t*)a.allowed;
   p.ldm = a.ld_allowed;
   if (a.graph && !a.graph->trivial) {  // (a trivial graph allows every label)
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev), "hipGetDevice");
+    if (a.graph->dev != dev)
+      return fail(TBS_EINVAL, "%s: the graph is on device %d, the call on device %d", who, a.graph->dev, dev);
     p.graph_rp = a.graph->rp;
     p.graph_label = a.graph->label;
     p.S = a.graph->S;

@@ -258,3 +258,16 @@ def test_with_joiner_log_probabilities():
     got = tbs.adjust_logits(logp, graph=graph, **a)
     csr = (np.asarray(graph_np.row_ptr), np.asarray(graph_np.label))
     check(got, *reference(logp, csr=csr, **a), True)
+
+
+def test_graph_on_another_device():
+    import torch
+    from paper_2211_00484_amd import synth, tbs
+    if torch.cuda.device_count() < 2:
+        pytest.skip("one device")
+    graph_np = synth.make_workload("graph", seed=0)[3]
+    graph = tbs.Graph.from_synth(graph_np)
+    with torch.cuda.device(1):
+        z = torch.zeros((2, graph.vocab_size), device="cuda:1")
+        with pytest.raises(tbs.TbsError, match="on device 0"):
+            tbs.adjust_logits(z, graph=graph, states=torch.zeros(2, dtype=torch.int32, device="cuda:1"))
