@@ -728,10 +728,11 @@ def _workspace(nbytes: int, like):
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
 
-def _rows32(n: int, name: str) -> int:
+def _size(n: int, name: str) -> int:
+    """n as an int32 argument (ctypes would drop its high bits)."""
     if n > _I32_MAX:
-        raise ValueError(f"{name}: {n} rows, at most {_I32_MAX}")
-    return n
+        raise ValueError(f"{name}: a dimension of {n}, at most {_I32_MAX}")
+    return int(n)
 
 
 def linear(x, weight, bias=None, residual=None, activation: str = "none",
@@ -747,9 +748,9 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none",
         code, act = _dtype_code(x), ACTIVATIONS[activation]
         if x.dim() == 0 or weight.dim() != 2:
             raise ValueError("x must be [..., K] and weight [N, K]")
-        N, K = (int(n) for n in weight.shape)
+        N, K = (_size(n, "weight") for n in weight.shape)
         x2, ldx = _matrix(x, x, K, "x")
-        M = _rows32(int(x2.shape[0]), "x")
+        M = _size(x2.shape[0], "x")
         w2, ldw = _matrix(weight, x, K, "weight")
         b = None if bias is None else _vector(bias, x, N, "bias")
         r, ldr = (None, 0) if residual is None else _matrix(residual, x, N, "residual", rows=M,
@@ -784,13 +785,13 @@ def linear_backward(grad_out, x, weight, pre=None, activation: str = "none",
         code, act = _dtype_code(grad_out), ACTIVATIONS[activation]
         if x.dim() == 0 or weight.dim() != 2 or grad_out.dim() == 0:
             raise ValueError("grad_out must be [..., N], x [..., K] and weight [N, K]")
-        N, K = (int(n) for n in weight.shape)
+        N, K = (_size(n, "weight") for n in weight.shape)
         if grad_out.shape[:-1] != x.shape[:-1]:
             raise ValueError("grad_out and x differ in their leading dimensions")
         if (act != 0) != (pre is not None):
             raise ValueError("pre goes with an activation, and only with one")
         g, ldg = _matrix(grad_out, grad_out, N, "grad_out")
-        M = _rows32(int(g.shape[0]), "grad_out")
+        M = _size(g.shape[0], "grad_out")
         x2, ldx = _matrix(x, grad_out, K, "x", rows=M)
         w2, ldw = _matrix(weight, grad_out, K, "weight")
         p, ldp = (None, 0) if pre is None else _matrix(pre, grad_out, N, "pre", rows=M)
@@ -829,9 +830,9 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
         code = _dtype_code(logits)
         if logits.dim() == 0 or logits.shape[-1] == 0:
             raise ValueError("logits must be [..., V]")
-        V, i32 = int(logits.shape[-1]), torch.int32
+        V, i32 = _size(logits.shape[-1], "logits"), torch.int32
         z, ldz = _matrix(logits, logits, V, "logits")
-        R = _rows32(int(z.shape[0]), "logits")
+        R = _size(z.shape[0], "logits")
         if (graph is None) != (states is None):
             raise ValueError("graph and states go together")
         a = Adjustments(repetition=float(repetition), presence=float(presence),
@@ -840,8 +841,9 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
         if history is not None:
             if history.dim() != 2:
                 raise ValueError("history must be [R, L]")
-            h, ldh = _matrix(history, logits, int(history.shape[1]), "history", i32, rows=R)
-            a.history, a.ld_history, a.history_cols = _ptr(h), ldh, int(h.shape[1])
+            cols = _size(history.shape[1], "history")
+            h, ldh = _matrix(history, logits, cols, "history", i32, rows=R)
+            a.history, a.ld_history, a.history_cols = _ptr(h), ldh, cols
             keep.append(h)
         elif history_lengths is not None or row_penalties is not None:
             raise ValueError("history_lengths and row_penalties go with a history")
@@ -890,7 +892,7 @@ def transducer_gradient(kind: str, blank, label, lengths, weights=None, stream=N
     import torch
     if blank.dim() != 3 or blank.shape[2] < 1:
         raise ValueError("blank must be [B, T, U + 1]")
-    B, T, U1 = (int(n) for n in blank.shape)
+    B, T, U1 = (_size(n, "blank") for n in blank.shape)
     U, f32 = U1 - 1, torch.float32
     if tuple(label.shape) != (B, T, U) or label.device != blank.device:
         raise ValueError("label must be [B, T, U] beside blank [B, T, U + 1]")

@@ -198,3 +198,20 @@ def test_binding_checks():
         tbs.transducer_gradient("standard", z(1, 2, 1025), z(1, 2, 1024), [[2, 3]])
     with pytest.raises(KeyError):
         tbs.linear(x, w, activation="swish")
+
+
+@pytest.mark.gpu
+def test_binding_refuses_sizes_beyond_int32():
+    """Each would be a small size in its low 32 bits (nothing here takes memory)."""
+    import torch
+    n = 2 ** 32 + 1
+    wide = lambda *s, **k: torch.zeros((1,), device="cuda", **k).expand(s)
+    i32 = dict(dtype=torch.int32)
+    for f in (lambda: tbs.linear(wide(1, n), wide(2, n)), lambda: tbs.linear(wide(1, 2), wide(n, 2)),
+              lambda: tbs.linear_backward(wide(1, 2), wide(1, n), wide(2, n)),
+              lambda: tbs.adjust_logits(wide(1, n)),
+              lambda: tbs.adjust_logits(wide(1, 9), history=wide(1, n, **i32)),
+              lambda: tbs.transducer_gradient("modified", wide(1, n, 2), wide(1, n, 1), [[1, 1]]),
+              lambda: tbs.transducer_gradient("modified", wide(1, 2, n + 1), wide(1, 2, n), [[1, 1]])):
+        with pytest.raises(ValueError, match="a dimension of"):
+            f()
