@@ -473,8 +473,9 @@ tbs_status tbs_linear(int32_t dtype, const void *x, int64_t ldx, const void *w, 
 /*
  * Gradients of tbs_linear from grad_out [M][N], the gradient of out:
  *   dz    [M][N] = grad_out * act'(pre): the gradient of the activation's argument, so of
- *         a residual added before it; rounded to the element type, as the products below
- *         take it.  Not written for TBS_ACT_NONE (dz is grad_out then);
+ *         a residual added before it.  Rounded to the element type where it is written; the
+ *         products below take it with twice that type's bits (where it is beyond the type's
+ *         range, as infinite).  Not written for TBS_ACT_NONE (dz is grad_out then);
  *   dx    [M][K] = dz w;  dw [N][K] = dz^T x;  dbias [N] = the sum of dz's rows.
  * (The gradient of a residual added after the activation is grad_out.)
  *   pre   [M][N] as tbs_linear wrote it; NULL for TBS_ACT_NONE.

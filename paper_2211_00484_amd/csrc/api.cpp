@@ -1952,6 +1952,10 @@ bool plan_dw(ProductArgs& p, int32_t dtype, int32_t M, int32_t N, int32_t K, boo
   p.rsum = dbias;
   return plan_product(p, dtype, false, false);
 }
+// Whether dz has bits that its rounding takes off: not in 32 bits, nor where slopes are 0 or 1.
+bool dz_in_two_parts(int32_t dtype, int32_t activation) {
+  return dtype != kF32 && activation != kActNone && activation != kActRelu;
+}
 void place_parts(ProductArgs& p, void* at) {
   p.part = (float*)at;
   p.rpart = p.part + (size_t)p.splits * p.M * p.N;
@@ -2033,11 +2037,12 @@ size_t tbs_linear_backward_workspace(int32_t dtype, int32_t activation, int32_t 
   if (!known_dtype(dtype) || M < 1 || N < 1 || K < 1) return 0;
   ProductArgs p;
   size_t parts = 0, dz = 0;
+  const size_t whole = align16((size_t)M * N * elem_size(dtype));
   if (want_dx && plan_dx(p, dtype, M, N, K)) parts = product_part_floats(p);
   if ((want_dw || want_dbias) && plan_dw(p, dtype, M, N, K, want_dw, want_dbias))
     parts = std::max(parts, product_part_floats(p));
-  if (activation != kActNone && !want_dz && (want_dx || want_dw || want_dbias))
-    dz = align16((size_t)M * N * elem_size(dtype));
+  if (activation != kActNone && (want_dx || want_dw || want_dbias))
+    dz = (want_dz ? 0 : whole) + (dz_in_two_parts(dtype, activation) ? whole : 0);
   return dz + parts * sizeof(float);  // (the products take turns at the parts)
 }
 
@@ -2068,15 +2073,21 @@ tbs_status tbs_linear_backward(int32_t dtype, const void* grad_out, int64_t ldg,
   char* parts = (char*)workspace;
   const void* g = grad_out;
   long long ld = ldg;
+  void* low = nullptr;
   if (act && M > 0 && (products || dz)) {
+    const size_t whole = align16((size_t)M * N * elem_size(dtype));
     void* to = dz;
     long long ldt = lddz;
     if (!dz) {
       to = workspace;
       ldt = N;
-      parts += align16((size_t)M * N * elem_size(dtype));
+      parts += whole;
     }
-    HIP_TRY(launch_act_grad(dtype, grad_out, ldg, pre, ldp, to, ldt, M, N, activation, st),
+    if (products && dz_in_two_parts(dtype, activation)) {
+      low = parts;
+      parts += whole;
+    }
+    HIP_TRY(launch_act_grad(dtype, grad_out, ldg, pre, ldp, to, ldt, low, N, M, N, activation, st),
             "launch(activation gradient)");
     g = to;
     ld = ldt;
@@ -2084,6 +2095,8 @@ tbs_status tbs_linear_backward(int32_t dtype, const void* grad_out, int64_t ldg,
   if (dx && M > 0) {
     pdx.a = g;
     pdx.lda = ld;
+    pdx.a_low = low;
+    pdx.lda_low = N;
     pdx.b = w;
     pdx.ldb = ldw;
     place_parts(pdx, parts);
@@ -2093,6 +2106,8 @@ tbs_status tbs_linear_backward(int32_t dtype, const void* grad_out, int64_t ldg,
   if (dw || dbias) {
     pdw.a = g;
     pdw.lda = ld;
+    pdw.a_low = low;
+    pdw.lda_low = N;
     pdw.b = dw ? x : g;  // dbias alone: any operand will do
     pdw.ldb = dw ? ldx : ld;
     pdw.rout = dbias;

@@ -377,6 +377,8 @@ struct ProductArgs {
   const void* a;            // rows of lda elements: of k for each m, or of m for each k
   const void* b;            // rows of ldb elements: of k for each n, or of n for each k
   long long lda, ldb;
+  const void* a_low;        // or null: what A's rounding to 16 bits took off (linear.hip), rows of
+  long long lda_low;        // lda_low
   int M, N, K;
   int shape;                // tile (plan_product)
   int tiles_m, tiles_n;
@@ -394,7 +396,7 @@ inline size_t product_part_floats(const ProductArgs& p) {
 }
 hipError_t launch_product(const ProductArgs& p, int dtype, bool akc, bool bkc, hipStream_t st);
 hipError_t launch_act_grad(int dtype, const void* dy, long long ldy, const void* pre, long long ldp, void* dz,
-                           long long ldz, int M, int N, int act, hipStream_t st);
+                           long long ldz, void* low, long long ldl, int M, int N, int act, hipStream_t st);
 
 // Adjusted logits (adjust.hip).
 struct AdjustArgs {

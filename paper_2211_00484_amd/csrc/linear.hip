@@ -6,8 +6,11 @@
 // its columns (W of dx, both operands of dW).  Sums are fp32 on the matrix units: bf16 and
 // fp16 operands by 16x16x32 products, fp32 operands by 16x16x4 products.
 //
-// dz is rounded to the element type before dx and dW, as a matrix instruction takes it: their
-// errors against 64 bits are then those of two roundings (1.4 times those of one).
+// dz of 16-bit layers is a product of its own and has more bits than a matrix instruction takes
+// of an operand: dx, dW and dbias take it in two parts of the element type, so that they are
+// rounded once, as the forward product is (from the rounded dz alone their errors are 1.4 times
+// those of one rounding, and dz below fp16's range is lost to the sums over rows).  It costs their
+// products twice (40,000 x 512, N = 500 bf16 with tanh 152 us, 100 from the rounded dz).
 //
 // Bound, MI355X: 16-bit, the matrix units (in the main loop of 128 x 128 tiles they are busy 86%
 // of its cycles, of 256 x 256 tiles 70%) and, for K of a few hundred, what is not the main loop:
@@ -342,13 +345,22 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// A 16-bit value's second part, what its rounding took off, is held times 2^kLowBits: fp16 has no
+// exponents to spare for it, bf16 has.
+template <class T>
+constexpr int kLowBits = 0;
+template <>
+constexpr int kLowBits<_Float16> = 11;
+
 // One workgroup: a BM x BN tile of C over slices [first, last) of one of `splits` parts of k;
 // each wave WM x WN of it.  splits > 1: fp32 partial sums to part [splits][M][N] (and, rsum,
 // the sums over k of A's rows to rpart [splits][M]); else the epilogue (rsum: to rout).
 // DIRECT: operands whose rows are 4-byte aligned are copied straight into a ring of ST
 // slices, ST - 1 of them in flight while one is used; the last slice, where it is not whole, and
 // other operands go through registers.
-template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT>
+// LOW: A is a + a_low 2^-kLowBits; the part's slices are gone through twice, those of a_low first,
+// whose sums are scaled before those of a are added.
+template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT, bool LOW>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductArgs p) {
   constexpr int THREADS = 64 * (BM / WM) * (BN / WN);
   constexpr int MB = WM / 16, NB = WN / 16;
@@ -415,62 +427,93 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
   };
   Stager<T, AKC, BM, THREADS> sa;
   Stager<T, BKC, BN, THREADS> sb;
+  const T* a_now = LOW ? (const T*)p.a_low : a;  // the part of A that is staged
+  long long lda_now = LOW ? p.lda_low : p.lda;
   auto load = [&](int s) {
-    sa.load(a, p.lda, m0, p.M, s * kSlice<T>, p.K);
+    sa.load(a_now, lda_now, m0, p.M, s * kSlice<T>, p.K);
     sb.load(b, p.ldb, n0, p.N, s * kSlice<T>, p.K);
   };
-  if (DIRECT) {
-    Copier<T, AKC, BM, THREADS> ca;
-    Copier<T, BKC, BN, THREADS> cb;
-    ca.init(a, p.lda, m0, p.M, first * kSlice<T>);
+  Copier<T, AKC, BM, THREADS> ca;
+  Copier<T, BKC, BN, THREADS> cb;
+  constexpr int kCopies = ca.N + cb.N;
+  const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
+  // slices that copies may take: all, but for a last one that is not whole
+  const bool partial = p.K % kSlice<T> != 0 || (!AKC && p.M % kChunkElems<T> != 0) ||
+                       (!BKC && p.N % kChunkElems<T> != 0);
+  const int whole = partial ? min(last, slices - 1) : last;
+  const int count = last - first, total = LOW ? 2 * count : count;  // turns: slices of either part
+  int in = 0;  // stage that the next turn's slice goes to
+  auto begin = [&]() {
+    ca.init(a_now, lda_now, m0, p.M, first * kSlice<T>);
     cb.init(b, p.ldb, n0, p.N, first * kSlice<T>);
-    constexpr int kCopies = ca.N + cb.N;
-    const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
-    // slices that copies may take: all, but for a last one that is not whole
-    const bool partial = p.K % kSlice<T> != 0 || (!AKC && p.M % kChunkElems<T> != 0) ||
-                         (!BKC && p.N % kChunkElems<T> != 0);
-    const int whole = partial ? min(last, slices - 1) : last;
-    int in = 0;  // stage that the next slice goes to
-    auto request = [&](int s) {
-      if (s < whole) {
-        ca.copy(base + in * kStage, wave);
-        cb.copy(base + in * kStage + kA, wave);
-      } else if (s < last) {
-        load(s);
-        sa.store(lds + in * kStage);
-        sb.store(lds + in * kStage + kA);
-      }
-      in = in == ST - 1 ? 0 : in + 1;
-    };
+  };
+  auto slice_of = [&](int turn) { return first + (LOW && turn >= count ? turn - count : turn); };
+  auto request = [&](int turn) {
+    if (LOW && turn == count) {
+      a_now = a;
+      lda_now = p.lda;
+      begin();
+    }
+    const int s = slice_of(turn);
+    if (s < whole && (!LOW || turn < total)) {
+      ca.copy(base + in * kStage, wave);
+      cb.copy(base + in * kStage + kA, wave);
+    } else if (turn < total) {
+      load(s);
+      sa.store(lds + in * kStage);
+      sb.store(lds + in * kStage + kA);
+    }
+    in = in == ST - 1 ? 0 : in + 1;
+  };
+  int turn = 0, out = 0;
+  if (DIRECT) {
+    begin();
 #pragma unroll
-    for (int i = 0; i < ST - 1; ++i) request(first + i);
-    int out = 0;
-    for (int s = first; s < last; ++s) {
-      if (s + ST - 2 < whole) wait_copies<(ST - 2) * kCopies>();
-      else wait_copies<0>();
-      request(s + ST - 1);  // (to the place of slice s - 1, which every wave has read)
-      slice(lds + out * kStage, s > first);
-      out = out == ST - 1 ? 0 : out + 1;
-    }
-  } else {
-    if (first < last) {
-      load(first);
-      sa.store(lds);
-      sb.store(lds + kA);
-    }
-    __syncthreads();
-    for (int s = first; s < last; ++s) {
-      char* next = lds + (~(s - first) & 1) * kStage;
-      if (s + 1 < last) load(s + 1);
-      slice(lds + ((s - first) & 1) * kStage, s > first);
-      if (s + 1 < last) {
-        sa.store(next);
-        sb.store(next + kA);
+    for (int i = 0; i < ST - 1; ++i) request(i);
+  }
+  for (int pass = LOW ? 1 : 0; pass >= 0; --pass) {
+    if (DIRECT) {
+      for (int s = first; s < last; ++s, ++turn) {
+        // (ST - 2 slices behind this one may be in flight, if the last of them was copied)
+        if (slice_of(turn + ST - 2) < whole && (!LOW || turn + ST - 2 < total)) wait_copies<(ST - 2) * kCopies>();
+        else wait_copies<0>();
+        request(turn + ST - 1);  // (to the place of the slice before, which every wave has read)
+        slice(lds + out * kStage, s > first);
+        out = out == ST - 1 ? 0 : out + 1;
+      }
+    } else {
+      if (LOW && pass == 0) {
+        a_now = a;
+        lda_now = p.lda;
+      }
+      if (first < last) {
+        load(first);
+        sa.store(lds);
+        sb.store(lds + kA);
       }
       __syncthreads();
+      for (int s = first; s < last; ++s) {
+        char* next = lds + (~(s - first) & 1) * kStage;
+        if (s + 1 < last) load(s + 1);
+        slice(lds + ((s - first) & 1) * kStage, s > first);
+        if (s + 1 < last) {
+          sa.store(next);
+          sb.store(next + kA);
+        }
+        __syncthreads();
+      }
+    }
+    if (kDeep && first < last) multiply(h1);
+    if (LOW && kLowBits<T> != 0 && pass == 1) {
+      constexpr float kScale = 1.f / (float)(1 << kLowBits<T>);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        rs[i] *= kScale;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] *= kScale;
+      }
     }
   }
-  if (kDeep && first < last) multiply(h1);
   if (rsum && lane < 16) {
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
@@ -664,11 +707,12 @@ __global__ __launch_bounds__(256) void k_join_parts(ProductArgs p) {
   }
 }
 
-// dz = dy act'(pre), 16 bytes a thread and turn.  Bound: memory (8,000 x 512 fp32 10.4 us, 4.7 TB/s).
+// dz = dy act'(pre), 16 bytes a thread and turn; low (rows of ldl), unless null: what dz's rounding
+// took off, times 2^kLowBits (0 where dz is beyond the type's range).  Bound: memory (8,000 x 512 fp32 10.4 us, 4.7 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void k_act_grad(const T* __restrict__ dy, long long ldy, const T* __restrict__ pre,
-                                                  long long ldp, T* __restrict__ dz, long long ldz, int M, int N,
-                                                  int act) {
+                                                  long long ldp, T* __restrict__ dz, long long ldz,
+                                                  T* __restrict__ low, long long ldl, int M, int N, int act) {
   constexpr int E = kChunkElems<T>;
   const int per = (N + E - 1) / E;
   const long long total = (long long)M * per;
@@ -677,14 +721,31 @@ __global__ __launch_bounds__(256) void k_act_grad(const T* __restrict__ dy, long
     const T* y = dy + (size_t)m * ldy + n;
     const T* z = pre + (size_t)m * ldp + n;
     T* o = dz + (size_t)m * ldz + n;
+    T* l = sizeof(T) == 2 && low ? low + (size_t)m * ldl + n : nullptr;
+    // (both parts go by one rounding: the compiler may round a product to fp16 without fp32 between,
+    // and another time with it, a step apart at a tie)
+    auto parts = [&](float d, T& r, T& rl) {
+      r = from_float<T>(d);
+      asm("" : "+v"(r));
+      const float t = d - to_float(r);
+      rl = from_float<T>(fabsf(t) < INFINITY ? t * (float)(1 << kLowBits<T>) : 0.f);
+    };
     if (n + E <= N) {
       const Vec<T, E> vy = load_vec<T, E>(y), vz = load_vec<T, E>(z);
-      Vec<T, E> r;
+      Vec<T, E> r, rl;
 #pragma unroll
-      for (int v = 0; v < E; ++v) r.v[v] = from_float<T>(to_float(vy.v[v]) * slope(to_float(vz.v[v]), act));
+      for (int v = 0; v < E; ++v) {
+        parts(to_float(vy.v[v]) * slope(to_float(vz.v[v]), act), r.v[v], rl.v[v]);
+      }
       store_vec(o, r);
+      if (l) store_vec(l, rl);
     } else {
-      for (int v = 0; n + v < N; ++v) o[v] = from_float<T>(to_float(y[v]) * slope(to_float(z[v]), act));
+      for (int v = 0; n + v < N; ++v) {
+        T r, rl;
+        parts(to_float(y[v]) * slope(to_float(z[v]), act), r, rl);
+        o[v] = r;
+        if (l) l[v] = rl;
+      }
     }
   }
 }
@@ -702,32 +763,40 @@ bool direct_ok(const void* p, long long ld, bool kc, int rows) {
          (kc || rows >= kChunkElems<T>);
 }
 
-template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT>
+template <class T, bool AKC, bool BKC, int BM, int BN, int WM, int WN, int ST, bool DIRECT, bool LOW>
 hipError_t launch_tile_d(const ProductArgs& p, hipStream_t st) {
   constexpr size_t lds = (DIRECT ? ST : 2) * (Layout<T, AKC, BM>::BYTES + Layout<T, BKC, BN>::BYTES);
   if (lds > 65536) {
     static LdsGrant grant;
-    const hipError_t e = grant((const void*)k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT>, lds);
+    const hipError_t e = grant((const void*)k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT, LOW>, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT>), dim3(p.tiles_m * p.tiles_n * p.splits),
+  hipLaunchKernelGGL((k_product<T, AKC, BKC, BM, BN, WM, WN, ST, DIRECT, LOW>), dim3(p.tiles_m * p.tiles_n * p.splits),
                      dim3(64 * (BM / WM) * (BN / WN)), lds, st, p);
   return hipGetLastError();
 }
 
-template <class T, bool AKC, bool BKC>
+template <class T, bool AKC, bool BKC, bool LOW>
 hipError_t launch_shape(const ProductArgs& p, hipStream_t st) {
-  const bool direct = direct_ok<T>(p.a, p.lda, AKC, p.M) && direct_ok<T>(p.b, p.ldb, BKC, p.N);
+  const bool direct = direct_ok<T>(p.a, p.lda, AKC, p.M) && direct_ok<T>(p.b, p.ldb, BKC, p.N) &&
+                      (!LOW || direct_ok<T>(p.a_low, p.lda_low, AKC, p.M));
   if (p.shape == 0)
-    return direct ? launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, true>(p, st)
-                  : launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, false>(p, st);
+    return direct ? launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, true, LOW>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 64, 64, 32, 32, 3, false, LOW>(p, st);
   if (p.shape == 1 || sizeof(T) == 4)
-    return direct ? launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, true>(p, st)
-                  : launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, false>(p, st);
+    return direct ? launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, true, LOW>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 128, 128, 64, 64, 2, false, LOW>(p, st);
   if constexpr (sizeof(T) == 2)
-    return direct ? launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, true>(p, st)
-                  : launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, false>(p, st);
+    return direct ? launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, true, LOW>(p, st)
+                  : launch_tile_d<T, AKC, BKC, 256, 256, 128, 64, 2, false, LOW>(p, st);
   return hipErrorInvalidValue;  // (not reached)
+}
+// (only gradients have an operand in two parts, and only 16-bit ones)
+template <class T, bool AKC>
+hipError_t launch_gradient(const ProductArgs& p, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (p.a_low) return launch_shape<T, AKC, false, true>(p, st);
+  return launch_shape<T, AKC, false, false>(p, st);
 }
 
 constexpr int kRowsShape = 3;
@@ -744,9 +813,9 @@ template <class T>
 hipError_t launch_product_t(const ProductArgs& p, bool akc, bool bkc, hipStream_t st) {
   if (p.shape == kRowsShape) return launch_rows<T>(p, st);
   hipError_t e;
-  if (akc && bkc) e = launch_shape<T, true, true>(p, st);
-  else if (akc) e = launch_shape<T, true, false>(p, st);
-  else e = launch_shape<T, false, false>(p, st);
+  if (akc && bkc) e = launch_shape<T, true, true, false>(p, st);
+  else if (akc) e = launch_gradient<T, true>(p, st);
+  else e = launch_gradient<T, false>(p, st);
   if (e != hipSuccess || p.splits == 1) return e;
   const long long items = (p.epi.out ? (long long)p.M * ((p.N + 3) / 4) : 0) + (p.rsum && p.rout ? p.M : 0);
   hipLaunchKernelGGL(k_join_parts<T>, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, st, p);
@@ -814,25 +883,25 @@ hipError_t launch_product(const ProductArgs& p, int dtype, bool akc, bool bkc, h
 
 template <class T>
 static hipError_t launch_act_grad_t(const void* dy, long long ldy, const void* pre, long long ldp, void* dz,
-                                    long long ldz, int M, int N, int act, hipStream_t st) {
+                                    long long ldz, void* low, long long ldl, int M, int N, int act, hipStream_t st) {
   const long long items = (long long)M * ((N + kChunkElems<T> - 1) / kChunkElems<T>);
   const long long blocks = std::min<long long>((items + 255) / 256, 1 << 20);
   hipLaunchKernelGGL(k_act_grad<T>, dim3((unsigned)blocks), dim3(256), 0, st, (const T*)dy, ldy, (const T*)pre, ldp,
-                     (T*)dz, ldz, M, N, act);
+                     (T*)dz, ldz, (T*)low, ldl, M, N, act);
   return hipGetLastError();
 }
 
 hipError_t launch_act_grad(int dtype, const void* dy, long long ldy, const void* pre, long long ldp, void* dz,
-                           long long ldz, int M, int N, int act, hipStream_t st) {
+                           long long ldz, void* low, long long ldl, int M, int N, int act, hipStream_t st) {
   if (M == 0 || N == 0) return hipSuccess;
-  if (ldy == N && ldp == N && ldz == N && (long long)M * N < (1ll << 30)) {  // one long row
+  if (ldy == N && ldp == N && ldz == N && (!low || ldl == N) && (long long)M * N < (1ll << 30)) {  // one long row
     N *= M;
     M = 1;
-    ldy = ldp = ldz = N;
+    ldy = ldp = ldz = ldl = N;
   }
-  if (dtype == kF32) return launch_act_grad_t<float>(dy, ldy, pre, ldp, dz, ldz, M, N, act, st);
-  if (dtype == kBF16) return launch_act_grad_t<bf16>(dy, ldy, pre, ldp, dz, ldz, M, N, act, st);
-  return launch_act_grad_t<_Float16>(dy, ldy, pre, ldp, dz, ldz, M, N, act, st);
+  if (dtype == kF32) return launch_act_grad_t<float>(dy, ldy, pre, ldp, dz, ldz, low, ldl, M, N, act, st);
+  if (dtype == kBF16) return launch_act_grad_t<bf16>(dy, ldy, pre, ldp, dz, ldz, low, ldl, M, N, act, st);
+  return launch_act_grad_t<_Float16>(dy, ldy, pre, ldp, dz, ldz, low, ldl, M, N, act, st);
 }
 
 }  // namespace tbs
