@@ -1083,7 +1083,10 @@ __global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank,
           sb = share(ca0[q], xb[q], cb0[q], rz, ez);
         }
         if (lab[q]) sl = share(ca0[q], xl[q], cb1[q], rz, ez);
-        if (bad) sb = sl = NAN;
+        if (bad) {
+          sb = NAN;
+          if (lab[q]) sl = NAN;
+        }
         sb = (float)(w * (double)sb);
         sl = (float)(w * (double)sl);
       }
