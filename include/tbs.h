@@ -418,7 +418,9 @@ tbs_status tbs_transducer_forward(int32_t kind, const float *blank, const float 
  *                   no longer tell its paths apart) and one with lengths out of range; NaN
  *                   inside the lengths of one whose total is NaN or above 1e8.  Scores are
  *                   held with fp32 mantissas and integer exponents (recursions in fp64), so
- *                   a gradient is within a few 1e-7 of itself however long the utterance;
+ *                   a gradient is within a few 1e-7 of itself however long the utterance.
+ *                   (Partial sums of a path below -1.86e8 count as no path, and above
+ *                   1.86e8 as NaN, also where later inputs lead back within the limits);
  *   workspace       DEVICE, 16-byte aligned, of at least the bytes that
  *                   tbs_transducer_gradient_workspace gives for B, T and U; contents on
  *                   entry are of no matter.  Calls that may overlap need one each.

@@ -239,22 +239,24 @@ constexpr float kLn2Hi = 0.69314575f, kLn2Lo = 1.42860677e-6f;  // ln 2, the fir
 
 __device__ __forceinline__ bool reachable(int2 c) { return c.y > kZeroExp / 2; }
 __device__ __forceinline__ int2 zero_cell() { return make_int2(__float_as_int(0.5f), kZeroExp); }
-// e^v; below 2^(kZeroExp / 2) it counts as 0, above 2^(-kZeroExp / 2) as infinite
+// e^v; below 2^(kZeroExp / 2) it counts as 0, above 2^(-kZeroExp / 2), or with v NaN, it is NaN
+__device__ __forceinline__ int2 nan_cell() { return make_int2(__float_as_int(NAN), 0); }
 __device__ __forceinline__ int2 log_to_cell(double v) {
   const double t = v * 1.4426950408889634;
   if (t <= (double)(kZeroExp / 2)) return zero_cell();
-  if (!(t < (double)(-kZeroExp / 2))) return make_int2(__float_as_int(v == v ? INFINITY : NAN), 0);
+  if (!(t < (double)(-kZeroExp / 2))) return nan_cell();
   const double e = floor(t) + 1.0;
   return make_int2(__float_as_int((float)exp2(t - e)), (int)e);
 }
 
 // What shares are taken of: the last cell's score z, which for eq. (1) leaves the last blank out
-// as beta does, unless the total with it is no number to divide by.
-template <int KIND>
+// as beta does.  The total decides whether there are any: none below -kMaxTotal, NaN above
+// kMaxTotal.  (Cells reach 2^(kZeroExp / 2), 1.86e8 as a logarithm, so that those of the paths
+// that make up a total within the limits have their scores.)
+constexpr double kMaxTotal = 1e8;
 __device__ __forceinline__ int2 likelihood_cell(int2 z, double total) {
-  if (KIND != 0) return z;
-  const int2 all = log_to_cell(total);
-  return reachable(all) && __int_as_float(all.x) < INFINITY ? z : all;
+  if (total < -kMaxTotal) return zero_cell();
+  return total <= kMaxTotal ? z : nan_cell();
 }
 
 // Row of blank that step row i reads, in either direction (eq. (1): for i > 0 only; eq. (3)
@@ -304,7 +306,7 @@ __device__ void log_scores(const float* __restrict__ bl, const float* __restrict
     double res = buf[(steps & 1) * U1 + Ub];
     const int2 z = log_to_cell(res);
     if (KIND == 0) res += (double)bl[(size_t)(Tb - 1) * U1 + Ub];
-    *zcell = likelihood_cell<KIND>(z, res);
+    *zcell = likelihood_cell(z, res);
     *total = res;
   }
 }
@@ -856,7 +858,7 @@ __global__ __launch_bounds__(kRingThreads, NW == 1 && (K > 8 || (K == 8 && KIND 
       if (!rev) {
         total[b] = res;
         if (status) status[b] = 0;
-        if (CELLS) zcell[b] = likelihood_cell<KIND>(make_int2(__float_as_int((float)mine), exp2), res);
+        if (CELLS) zcell[b] = likelihood_cell(make_int2(__float_as_int((float)mine), exp2), res);
       }
     }
   }
@@ -990,17 +992,24 @@ __global__ __launch_bounds__(kRingThreads) void k_scores_logs(
   else log_scores<KIND, false>(bl, lb, Tb, Ub, U, c, buf, total + b, zcell + b);
 }
 
-// e^x = (what is returned) 2^k
-__device__ __forceinline__ float exp_parts(float x, int& k) {
-  const float xc = fminf(fmaxf(x, -1e8f), 1e8f);  // (beyond it what it leads to is 0 or infinite)
-  const float r = rintf(xc * 1.44269504f);
-  k = (int)r;
-  return __expf(__builtin_fmaf(-r, kLn2Lo, __builtin_fmaf(-r, kLn2Hi, x == x ? xc : x)));
+// e^x = (what is returned) 2^k; x = -inf is the caller's.  In fp32 the product r ln 2 that is taken
+// off x keeps its digits up to r of 2^15 (r has 15 bits and the first part of ln 2 16; the
+// second's own error, 2^-44, times r is 2^-29); larger x are reduced in fp64.  Beyond 2^40 there
+// is no score left for k to meet.
+__device__ __forceinline__ float exp_parts(float x, long long& k) {
+  if (fabsf(x) < 16384.f) {
+    const float r = rintf(x * 1.44269504f);
+    k = (int)r;
+    return __expf(__builtin_fmaf(-r, kLn2Lo, __builtin_fmaf(-r, kLn2Hi, x)));
+  }
+  const double t = fmin(fmax((double)x * 1.4426950408889634, -0x1p40), 0x1p40), f = floor(t);
+  k = (long long)f;
+  return x == x ? exp2f((float)(t - f)) : x;
 }
 // a e^x b / z for cells a and b (0 if one is unreachable or x is -inf); rz: 1 / z's mantissa
-__device__ __forceinline__ float share(int2 a, float x, int2 b, float rz, int ez) {
+__device__ __forceinline__ float share(int2 a, float x, int2 b, float rz, long long ez) {
   if (!reachable(a) || !reachable(b) || x == -INFINITY) return 0.f;
-  int k;
+  long long k;
   const float m = exp_parts(x, k) * __int_as_float(a.x) * __int_as_float(b.x) * rz;
   const long long e = (long long)a.y + b.y - ez + k;
   return ldexpf(m, (int)(e < -400 ? -400 : e > 400 ? 400 : e));
@@ -1023,7 +1032,7 @@ __global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank,
   const float zm = __int_as_float(zc.x);
   const bool bad = !(zm < INFINITY);
   float rz = 1.f / zm;
-  int ez = zc.y;
+  long long ez = zc.y;
   const double w = weights ? weights[b] : 1.0;
   const int2* ca = cells + (size_t)2 * b * n;
   const int2* cb = ca + n;
@@ -1032,7 +1041,7 @@ __global__ __launch_bounds__(256) void k_shares(const float* __restrict__ blank,
   float* gb = grad_blank + (size_t)b * n;
   float* gl = grad_label + (size_t)b * T * U;
   if (KIND == 2 && live) {  // the last blank, a factor of g
-    int k;
+    long long k;
     rz *= exp_parts(bl[(size_t)(Tb - 1) * U1 + Ub], k);
     ez -= k;
   }
