@@ -91,6 +91,9 @@ __device__ __forceinline__ float activate(float z, int act) {
     default: return z;
   }
 }
+// z, but for values so large that what a slope multiplies them by is 0: an infinite z, which pre
+// holds where the type's range ends, has its limit too.
+__device__ __forceinline__ float limited(float z) { return fabsf(z) > 1e4f ? copysignf(1e4f, z) : z; }
 __device__ __forceinline__ float slope(float z, int act) {
   switch (act) {
     case kActRelu: return z <= 0.f ? 0.f : 1.f;
@@ -101,12 +104,12 @@ __device__ __forceinline__ float slope(float z, int act) {
     }
     case kActSilu: {
       const float s = sigmoid_f32(z);
-      return s * (1.f + z * (1.f - s));
+      return s * (1.f + limited(z) * (1.f - s));
     }
     case kActGelu: {
       float density;
       const float cdf = normal_cdf(z, density);
-      return cdf + z * 0.39894228f * density;
+      return cdf + limited(z) * 0.39894228f * density;
     }
     default: return 1.f;
   }

@@ -49,3 +49,30 @@ def test_gelu_tails(dtype):
     over = (slope.double() - want).abs() - e - _half(dt) * (want.abs() + e)
     i = over.argmax()
     assert over.max() <= 0, (z[i].item(), slope[i].item(), want[i].item())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("act", ["relu", "tanh", "silu", "gelu"])
+def test_slopes_of_infinite_arguments(act, dtype):
+    """pre beyond the type's range is infinite: its slope is the activation's limit, 0 or 1, and a
+    NaN's is NaN (relu's is 1)."""
+    import torch
+    from paper_2211_00484_amd import tbs
+    dt = _t(dtype)
+    z = torch.tensor([math.inf, -math.inf, math.nan, torch.finfo(dt).max, torch.finfo(dt).min], dtype=dt,
+                     device="cuda")
+    slope = _through(z, act)[1].float().cpu().tolist()
+    high = 0.0 if act == "tanh" else 1.0
+    assert slope[:2] == [high, 0.0] and slope[3:] == [high, 0.0]
+    assert slope[2] == 1.0 if act == "relu" else math.isnan(slope[2])
+    if dtype != "float16":
+        return
+    # as a layer meets it: sums of 100,000 either way
+    x = torch.tensor([[250.0], [-250.0]], dtype=dt, device="cuda")
+    w = torch.full((3, 1), 400.0, dtype=dt, device="cuda")
+    out, pre = tbs.linear(x, w, activation=act, want_pre=True)
+    assert torch.isinf(pre).all()
+    g = torch.ones((2, 3), dtype=dt, device="cuda")
+    got = tbs.linear_backward(g, x, w, pre=pre, activation=act, want_pre=True)
+    assert (got.pre[0] == high).all() and (got.pre[1] == 0).all()
+    assert (got.bias == high).all() and (got.x[1] == 0).all() and (got.x[0] == high * 1200).all()
