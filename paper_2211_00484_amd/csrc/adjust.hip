@@ -36,8 +36,13 @@ struct LogSum {
     s = (m == mm ? s : s * __expf(m - mm)) + (o.m == mm ? o.s : o.s * __expf(o.m - mm));
     m = mm;
   }
-  // its logarithm; 0 for an empty sum, whose terms are all -inf and stay so
-  __device__ __forceinline__ float log() const { return m == ninff() && s == 0.f ? 0.f : m + logf(s); }
+  // log of e^x over it, for x a term that is not -inf (an empty sum has none): x - m loses little or
+  // nothing, as m + log(s) would where m is large
+  struct Log {
+    float m, logs;
+    __device__ __forceinline__ float of(float x) const { return (x - m) - logs; }
+  };
+  __device__ __forceinline__ Log log() const { return Log{m, logf(s)}; }
 };
 
 __device__ __forceinline__ LogSum workgroup_sum(LogSum v, LogSum* red) {
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_adjust(AdjustArgs p) {
       sum.m = fmaxf(sum.m, x);
     }
   }
-  float shift = 0.f;
+  LogSum::Log norm{0.f, 0.f};
   if (PASS == kSums || (PASS == kDirect && p.normalize)) {
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void k_adjust(AdjustArgs p) {
       if (tid == 0) p.stats[(size_t)r * p.parts + part] = make_float2(sum.m, sum.s);
       return;
     }
-    shift = sum.log();
+    norm = sum.log();
   }
   if (PASS == kApply) {
     LogSum all{ninff(), 0.f};
@@ -182,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void k_adjust(AdjustArgs p) {
       const float2 s = p.stats[(size_t)r * p.parts + i];
       all.add(LogSum{s.x, s.y});
     }
-    shift = workgroup_sum(all, red).log();
+    norm = workgroup_sum(all, red).log();
   }
   T* out = (T*)p.out + (size_t)r * p.ldo + c0;
 #pragma unroll
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void k_adjust(AdjustArgs p) {
     const int c = (q * kThreads + tid) * E;
     Vec<T, E> o;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o.v[e] = from_float<T>(v[q][e] == ninff() ? ninff() : v[q][e] - shift);
+    for (int e = 0; e < E; ++e) o.v[e] = from_float<T>(v[q][e] == ninff() ? ninff() : norm.of(v[q][e]));
     if (c + E <= n) {
       store_vec(out + c, o);
     } else {
