@@ -866,7 +866,8 @@ bool plan_product(ProductArgs& p, int dtype, bool akc, bool bkc) {
   const int cus = device_cus() > 0 ? device_cus() : 256;
   p.splits = 1;
   // (64 rows, K = 2,048: 12.2 us by rows, 7.7 by tiles in parts; 16 rows, K = 512, N = 5,000 4.0)
-  if (akc && bkc && (p.M <= 16 || (p.M <= 32 && p.K <= 1024))) {
+  // (a workgroup per 16 columns, so that a launch takes a quarter of the columns that tiles would)
+  if (akc && bkc && (p.M <= 16 || (p.M <= 32 && p.K <= 1024)) && (p.N + 15) / 16 <= kMaxTiles) {
     p.shape = kRowsShape;
     p.tiles_m = 1;
     p.tiles_n = (p.N + 15) / 16;
