@@ -537,13 +537,19 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
       }
     }
     if (kDeep && first < last) multiply(h1);
-    if (LOW && kLowBits<T> != 0 && pass == 1) {
+    if (LOW && pass == 1) {
+      // (an infinity or NaN of the other operand comes again with a, and with a's sign)
       constexpr float kScale = 1.f / (float)(1 << kLowBits<T>);
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
         rs[i] *= kScale;
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] *= kScale;
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float t = acc[i][j][v] * kScale;
+            acc[i][j][v] = fabsf(t) < INFINITY ? t : 0.f;
+          }
       }
     }
   }

@@ -123,3 +123,45 @@ def test_rows_of_their_own(dtype):
             s = _slope64(pre.double(), "tanh") * g.double()
             e = 2e-6 * g.double().abs()
             _within(dz[:, :N], s, e + _half(x.dtype) * (s.abs() + e) + _tiny(x.dtype), "dz")
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("act", SMOOTH)
+@pytest.mark.parametrize("M,K,N", [(5, 100, 37), (130, 100, 70), (3000, 64, 66)])
+def test_special_values(M, K, N, act, dtype):
+    """Infinities and NaN in grad_out, w and x reach what the formula takes them to, with their
+    signs, and nothing else."""
+    import math
+    import torch
+    from paper_2211_00484_amd import tbs
+    g, x, w, pre = _inputs(M, K, N, dtype, 3)
+    run = lambda g, x, w: tbs.linear_backward(g, x, w, pre=pre, activation=act, want_pre=True)
+    ref = run(g, x, w)
+    assert (ref.pre != 0).all()
+    sign = ref.pre.double().sign()
+
+    g2 = g.clone()
+    g2[2, N - 1], g2[1, 0] = math.nan, math.inf
+    got = run(g2, x, w)
+    keep = [m for m in range(M) if m not in (1, 2)]
+    assert torch.equal(got.x[keep], ref.x[keep]) and torch.isnan(got.x[2]).all()
+    up = _slope64(pre[1:2, :1].double(), act).sign().item()
+    assert torch.equal(got.x[1].double(), math.inf * up * w[0].double().sign())
+    assert torch.equal(got.weight[1:N - 1], ref.weight[1:N - 1]) and torch.isnan(got.weight[N - 1]).all()
+    assert torch.equal(got.weight[0].double(), math.inf * up * x[1].double().sign())
+    assert torch.equal(got.bias[1:N - 1], ref.bias[1:N - 1]) and torch.isnan(got.bias[N - 1])
+    assert got.bias[0].item() == math.inf * up
+
+    w2 = w.clone()
+    w2[N - 1, K - 1], w2[N - 2, 0] = math.inf, math.nan
+    got = run(g, x, w2)
+    assert torch.equal(got.x[:, 1:K - 1], ref.x[:, 1:K - 1]) and torch.isnan(got.x[:, 0]).all()
+    assert torch.equal(got.x[:, K - 1].double(), math.inf * sign[:, N - 1])
+    assert torch.equal(got.weight, ref.weight) and torch.equal(got.bias, ref.bias)
+
+    x2 = x.clone()
+    x2[1, 0], x2[3, K - 1] = -math.inf, math.nan
+    got = run(g, x2, w)
+    assert torch.equal(got.weight[:, 1:K - 1], ref.weight[:, 1:K - 1]) and torch.isnan(got.weight[:, K - 1]).all()
+    assert torch.equal(got.weight[:, 0].double(), -math.inf * sign[1])
+    assert torch.equal(got.x, ref.x) and torch.equal(got.bias, ref.bias)
