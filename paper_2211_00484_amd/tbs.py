@@ -676,10 +676,11 @@ def _dtype_code(t) -> int:
     return code
 
 
-def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False):
+def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False, lead=()):
     """(2-D tensor, row length) of ``t`` [..., cols]: a view where its rows are contiguous
     and no closer than their width, else a copy.  With one_row, a [cols] or [1, cols] tensor
-    stands for all rows (row length 0)."""
+    stands for all rows (row length 0).  lead: the leading dimensions that the rows stand for;
+    those of ``t``, if both have several, must be the same."""
     dtype = dtype or like.dtype
     if t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
@@ -694,6 +695,8 @@ def _matrix(t, like, cols: int, name: str, dtype=None, rows=None, one_row=False)
     n = m.shape[0]
     if rows is not None and n != rows and not (one_row and n == 1):
         raise ValueError(f"{name} must have {rows} rows, not {n}")
+    if len(lead) > 1 and len(shape) > 2 and shape[:-1] != lead and not (one_row and n == 1):
+        raise ValueError(f"{name} must have the leading dimensions {tuple(lead)}, not {tuple(shape[:-1])}")
     if cols > 1 and m.stride(1) != 1:
         m = m.contiguous()
     if one_row and (n == 1 or m.stride(0) == 0):
@@ -754,7 +757,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none",
         w2, ldw = _matrix(weight, x, K, "weight")
         b = None if bias is None else _vector(bias, x, N, "bias")
         r, ldr = (None, 0) if residual is None else _matrix(residual, x, N, "residual", rows=M,
-                                                            one_row=True)
+                                                            one_row=True, lead=x.shape[:-1])
         out = torch.empty(x.shape[:-1] + (N,), dtype=x.dtype, device=x.device)
         pre = torch.empty_like(out) if want_pre else None
         L = lib()
@@ -794,7 +797,8 @@ def linear_backward(grad_out, x, weight, pre=None, activation: str = "none",
         M = _size(g.shape[0], "grad_out")
         x2, ldx = _matrix(x, grad_out, K, "x", rows=M)
         w2, ldw = _matrix(weight, grad_out, K, "weight")
-        p, ldp = (None, 0) if pre is None else _matrix(pre, grad_out, N, "pre", rows=M)
+        p, ldp = (None, 0) if pre is None else _matrix(pre, grad_out, N, "pre", rows=M,
+                                                       lead=grad_out.shape[:-1])
         like = dict(dtype=grad_out.dtype, device=grad_out.device)
         dx = torch.empty(x.shape, **like) if want_x else None
         dw = torch.empty((N, K), **like) if want_weight else None
@@ -832,7 +836,7 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
             raise ValueError("logits must be [..., V]")
         V, i32 = _size(logits.shape[-1], "logits"), torch.int32
         z, ldz = _matrix(logits, logits, V, "logits")
-        R = _size(z.shape[0], "logits")
+        R, lead = _size(z.shape[0], "logits"), logits.shape[:-1]
         if (graph is None) != (states is None):
             raise ValueError("graph and states go together")
         a = Adjustments(repetition=float(repetition), presence=float(presence),
@@ -851,16 +855,18 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
             keep.append(_vector(history_lengths, logits, R, "history_lengths", i32))
             a.history_lengths = _ptr(keep[-1])
         if row_penalties is not None:
-            rp, _ = _matrix(row_penalties, logits, 3, "row_penalties", torch.float32, rows=R)
+            rp, _ = _matrix(row_penalties, logits, 3, "row_penalties", torch.float32, rows=R,
+                            lead=lead)
             keep.append(rp.contiguous())
             a.row_penalties = _ptr(keep[-1])
         if bias is not None:
-            m, a.ld_bias = _matrix(bias, logits, V, "bias", torch.float32, rows=R, one_row=True)
+            m, a.ld_bias = _matrix(bias, logits, V, "bias", torch.float32, rows=R, one_row=True,
+                                   lead=lead)
             a.bias = _ptr(m)
             keep.append(m)
         if allowed is not None:
             m, a.ld_allowed = _matrix(allowed, logits, (V + 31) // 32, "allowed", i32, rows=R,
-                                      one_row=True)
+                                      one_row=True, lead=lead)
             a.allowed = _ptr(m)
             keep.append(m)
         if graph is not None:
