@@ -345,12 +345,10 @@ hipError_t launch_transducer_forward(int kind, const float* blank, const float* 
 // transducer_probs bytes behind it.
 inline size_t transducer_cells(int B, int T, int U) { return (size_t)2 * B * T * (U + 1); }
 inline size_t transducer_zcells(int B) { return (size_t)(B + 1) / 2 * 2; }
-// exponentials of the inputs and flags of each utterance's parts, for batches that may run with
-// several chain waves (a workgroup per utterance and direction on at most 256 CUs)
+// bytes of the inputs' exponentials and the flags of each utterance's parts, where one of the kinds
+// may run with the chain waves that take them
 constexpr int kTransducerProbParts = 128;
-inline size_t transducer_probs(int B, int T, int U) {
-  return B <= 128 ? (size_t)B * T * (2 * (size_t)U + 1) * sizeof(double) + (size_t)B * kTransducerProbParts * sizeof(int) : 0;
-}
+size_t transducer_probs(int B, int T, int U);
 hipError_t launch_transducer_gradient(int kind, const float* blank, const float* label, const int* lengths,
                                       const double* weights, int B, int T, int U, double* total,
                                       float* grad_blank, float* grad_label, int* status, int2* cells,

@@ -1165,6 +1165,14 @@ hipError_t launch_gradient(const float* blank, const float* label, const int* le
 
 }  // namespace
 
+// (by the plan of a device of 256 CUs, the most that it goes by: fewer run fewer batches so)
+size_t transducer_probs(int B, int T, int U) {
+  if (B > 128) return 0;
+  const RingPlan p = plan_chain_waves(2 * B, T, U, 256);
+  if (!ring_takes_probs(p.K, p.NW)) return 0;
+  return (size_t)B * T * (2 * (size_t)U + 1) * sizeof(double) + (size_t)B * kTransducerProbParts * sizeof(int);
+}
+
 hipError_t launch_transducer_gradient(int kind, const float* blank, const float* label, const int* lengths,
                                       const double* weights, int B, int T, int U, double* total,
                                       float* grad_blank, float* grad_label, int* status, int2* cells,
