@@ -423,6 +423,10 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
     for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const bool rsum = !AKC && p.rsum && tn == 0 && wn == 0;
+  // fp32: the sums of half slices are added in fp64 (each by the next, so that nothing waits for
+  // it): a column of 64,000 in one fp32 sum is off by 4e-6, which 16-bit results do not show
+  constexpr bool kWide = sizeof(T) == 4;
+  double rt[MB] = {};
   // The fragments of a half slice, and their products.  The second half's products are left
   // until the first half of the next slice has been asked for, so that its LDS reads (and the
   // wait for the workgroup before them) have products to hide behind.
@@ -443,7 +447,13 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
       for (int i = 0; i < MB; ++i) acc[i][j] = mma(T{}, f.b[j], f.a[i], acc[i][j]);
     if (!AKC && rsum) {
 #pragma unroll
-      for (int i = 0; i < MB; ++i) rs[i] = mma(T{}, ones_fragment(T{}), f.a[i], rs[i]);
+      for (int i = 0; i < MB; ++i) {
+        if (kWide) {
+          rt[i] += (double)rs[i][0];
+          rs[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        rs[i] = mma(T{}, ones_fragment(T{}), f.a[i], rs[i]);
+      }
     }
   };
   constexpr bool kDeep = MB * NB <= 16;  // (larger tiles have no registers for two halves)
@@ -558,8 +568,9 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void k_product(ProductA
     for (int i = 0; i < MB; ++i) {
       const int m = m0 + wm + 16 * i + lane;
       if (m >= p.M) continue;
-      if (p.splits > 1) p.rpart[(size_t)split * p.M + m] = rs[i][0];
-      else if (p.rout) ((T*)p.rout)[m] = from_float<T>(rs[i][0]);
+      const float r = kWide ? (float)(rt[i] + (double)rs[i][0]) : rs[i][0];
+      if (p.splits > 1) p.rpart[(size_t)split * p.M + m] = r;
+      else if (p.rout) ((T*)p.rout)[m] = from_float<T>(r);
     }
   }
   if (!p.epi.out) return;
@@ -740,9 +751,9 @@ __global__ __launch_bounds__(256) void k_join_parts(ProductArgs p) {
   }
   id -= total;
   if (p.rsum && p.rout && id < p.M) {
-    float r = 0.f;
-    for (int s = 0; s < p.splits; ++s) r += p.rpart[(size_t)s * p.M + id];
-    ((T*)p.rout)[id] = from_float<T>(r);
+    double r = 0.0;
+    for (int s = 0; s < p.splits; ++s) r += (double)p.rpart[(size_t)s * p.M + id];
+    ((T*)p.rout)[id] = from_float<T>((float)r);
   }
 }
 
