@@ -526,6 +526,8 @@ tbs_status tbs_linear_backward(int32_t dtype, const void *grad_out, int64_t ldg,
  *   workspace      DEVICE, 16-byte aligned, of at least tbs_adjust_logits_workspace bytes
  *                  (0: none, may be NULL; none without normalize); calls that may overlap
  *                  need one each.
+ * A history of a transducer's labels holds no blank, so that penalties favour blank over
+ * every label that was given; a negative bias[0] counters that.
  * R >= 0 (0 is a no-op).  Errors: TBS_EINVAL for an unknown dtype, sizes, NULL pointers, row
  * lengths below the width, penalties out of range, a graph of another vocabulary or device or
  * a workspace that is too small; TBS_ECAPACITY for V > 2^30 or more rows than

@@ -7,11 +7,12 @@
 // bits of its state's arcs are gathered in LDS, from which each lane takes its columns'.  The
 // history and the arcs are read again by each workgroup of a row, for the columns of its own.
 // Bound: memory (a logit is read and written once; MI355X, 2,048 x 5,000 fp32 with a history of 120,
-// a graph and the log-softmax 22 us, 3.8 TB/s), the scan of long histories (512 x 46,340 bf16
-// with 2,000 labels each 38 us, 2.6 TB/s), and for few rows latency: state, arc range, arcs, and
-// the history are dependent round trips (128 x 500 4.6 us).  A log-softmax over more columns than a
-// workgroup holds takes two passes: sums first, then everything again with the row's
-// normaliser.
+// a graph and the log-softmax 22 us: 82 MB, which repeated passes find in part in the last-level
+// cache), the scan of long histories (512 x 46,340 bf16 with up to 2,000 labels each 37 us, 23
+// without), and for few rows latency: state, arc range, arcs, and the history are dependent round
+// trips (128 x 500 4.6 us).  A log-softmax over more columns than a workgroup holds takes two
+// passes: sums first, then everything again with the row's normaliser (512 x 46,340 bf16 48 us, 23
+// without it).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -214,7 +215,8 @@ hipError_t launch_pass(const AdjustArgs& p, hipStream_t st) {
     hipLaunchKernelGGL((k_adjust<T, decltype(q)::value, PASS>), grid, block, 0, st, p);
     return hipGetLastError();
   };
-  // (a whole row takes what it needs: 2,048 x 5,000 fp32 28 us by 8 accesses, 25 by 5)
+  // (a whole row takes what it needs: 2,048 x 5,000 fp32 28 us by 8 accesses, 25 by 5; seven go by
+  // eight, whose last is the one that is left out)
   const int q = (p.per - 1) / one + 1;
   if (q == 1) return launch(std::integral_constant<int, 1>());
   if (q == 2) return launch(std::integral_constant<int, 2>());

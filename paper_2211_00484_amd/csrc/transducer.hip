@@ -231,7 +231,9 @@ __global__ __launch_bounds__(kRingThreads) void k_transducer_logs(
 // (eq. 1, 2; for eq. (1) the cell's own, its last blank left out as a factor of all) or
 // T_b - 2 - i (eq. 3, whose last blank is a factor too).  So one kernel computes both, a
 // workgroup per utterance and direction, and a second one the shares.  A score is kept as
-// m 2^e (m a float in [0.5, 1]), so that shares lose nothing to the size of the scores.
+// m 2^e (m a float in [0.5, 1]), so that shares lose nothing to the size of the scores; the float
+// (8 bytes a cell with its exponent, where a double takes 12 or 16 of the memory that bounds the
+// second kernel) and products in fp32 leave a share 7e-8 (rms) off, where its own rounding is 2.5e-8.
 
 constexpr int kZeroExp = -(1 << 29);  // exponent of an unreachable cell; any below half of
                                       // it counts as one

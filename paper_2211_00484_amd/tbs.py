@@ -782,7 +782,8 @@ def linear_backward(grad_out, x, weight, pre=None, activation: str = "none",
                     want_x: bool = True, want_weight: bool = True, want_bias: bool = True,
                     want_pre: bool = False, stream=None) -> LinearGrads:
     """Gradients of ``linear`` (tbs_linear_backward) from grad_out [..., N], its x and weight,
-    and, unless the activation is "none", the pre it returned."""
+    and, unless the activation is "none", the pre it returned.  Each is rounded once; autograd
+    does not see the call."""
     import torch
     with _scope(grad_out, stream):
         code, act = _dtype_code(grad_out), ACTIVATIONS[activation]
@@ -828,7 +829,9 @@ def adjust_logits(logits, history=None, history_lengths=None, repetition: float 
     in place of the three numbers; bias float32 [V] or [R, V]; allowed int32 [W] or [R, W],
     W = (V + 31) // 32: bit v % 32 of word v // 32 allows label v; graph and states int32
     [R]: only blank and the labels on arcs out of each row's state (-1: no such mask).
-    out: a tensor like logits, or logits itself."""
+    out: a tensor like logits, or logits itself.  A history of a transducer's labels holds no
+    blank, so that penalties favour blank over every label that was given; a negative bias[0]
+    counters that.  Autograd does not see the call."""
     import torch
     with _scope(logits, stream):
         code = _dtype_code(logits)
@@ -894,7 +897,8 @@ def transducer_gradient(kind: str, blank, label, lengths, weights=None, stream=N
     sum(weights * total) with respect to blank and label (tbs_transducer_gradient); weights
     float64 [B] (None: 1 each).  Returns (total [B] float64, grad_blank [B, T, U+1],
     grad_label [B, T, U] float32, status [B] int32); gradients are 0 outside each utterance's
-    lengths.  lengths as a device int32 tensor [B, 2] costs no host copy."""
+    lengths.  lengths as a device int32 tensor [B, 2] costs no host copy.  The gradients are
+    results: autograd does not see the call."""
     import torch
     if blank.dim() != 3 or blank.shape[2] < 1:
         raise ValueError("blank must be [B, T, U + 1]")
